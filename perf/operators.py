@@ -304,13 +304,14 @@ def prepare(case, seed):
         import paper_2607_23250_amd as pl
         s["pl"] = pl
         sizes = (len(tiles), len(lengths), rows, keys, h_q, h_kv, d)
+        mask = dict(window=case["window"], sinks=case["sinks"])
         need = 0
         if case["op"] in ("fwd", "step"):
-            need = pl.libra_attn_window_workspace_size(*sizes, False)
+            need = pl.libra_attn_window_workspace_size(*sizes, False, **mask)
         if case["op"] == "bwd":
-            need = pl.libra_attn_window_workspace_size(*sizes, True)
+            need = pl.libra_attn_window_workspace_size(*sizes, True, **mask)
         if case["op"] in ("bwd_ckpt", "step"):
-            need = max(need, pl.libra_attn_bwd_ckpt8_workspace_size(*sizes, window=case["window"]))
+            need = max(need, pl.libra_attn_bwd_ckpt8_workspace_size(*sizes, **mask))
         s["ws"] = pl.alloc_workspace(need, DEV)
         # buffers that a program keeps over its layers
         s["out"] = torch.zeros((rows, h_q, d), dtype=torch.bfloat16, device=DEV)
