@@ -10,7 +10,11 @@
  *
  *   libra_plan      host, integer: tiles, costs and the placement;
  *   libra_attn_fwd  device: O and the log-sum-exp for a list of tiles;
- *   libra_attn_bwd  device: dQ, dK, dV for the same tiles.
+ *   libra_attn_bwd  device: dQ, dK, dV for the same tiles;
+ *   libra_attn_window_fwd, libra_attn_window_bwd  device: the same with a
+ *                   sliding window and first tokens that stay visible;
+ *   libra_ckpt8_pack, libra_ckpt8_unpack, libra_attn_bwd_ckpt8  device:
+ *                   activations held in 8 bits, and the backward from them.
  *
  * Conventions shared by every entry point
  *   - Return 0 (LIBRA_OK) or a negative LIBRA_E* code; nothing throws across
@@ -283,9 +287,112 @@ int libra_attn_bwd(const void *q, const void *k, const void *v, const void *o, c
                    void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Windowed attention: libra_attn_fwd and libra_attn_bwd with a sliding window
+ * and sinks.  The row at sample-local position p attends, of its own sample,
+ * the keys
+ *     { k <= p : k > p - window or k < sinks },
+ * its own key, the window - 1 before it and the sample's first `sinks` keys.
+ * O, LSE, dQ, dK and dV are those of libra_attn_fwd / libra_attn_bwd under
+ * this mask.  A row always attends its own key, so no row is empty; a window
+ * of at least the longest sample gives causal attention.
+ *   window >= 1; 0 <= sinks <= 1024 (EUNSUPPORTED above).  Values past
+ *       n_kv_rows act as n_kv_rows.  The backward takes those of the forward.
+ *   All other arguments, layouts, flags, errors, the handling of tiles that
+ *       are out of range and the timing records: as in libra_attn_fwd and
+ *       libra_attn_bwd.
+ *   workspace: >= libra_attn_window_workspace_size bytes for the same window,
+ *       sinks and direction, 256-byte aligned (0 bytes: invalid sizes).
+ * Single tokens: a tile may be one row.  For a batch of cached sequences,
+ * cu_seqlens holds the sequences' places in k and v, and each has one tile of
+ * its newest position.  A sequence's place may be longer than what it holds:
+ * keys past a tile's last row (of the forward's work item, at most 128 rows)
+ * are not read.
+ * Inputs: k and v must be finite from a sample's first key to the last row
+ * that the tiles cover in it, and q, o, lse and dout in the covered
+ * (row, head) pairs; nothing else is used.
+ * Split K: a call with fewer than two work items per workgroup cuts items of
+ * 8 or more 64-key blocks into key ranges as libra_attn_fwd does.  dK / dV of
+ * sink keys are summed over parts of a long sample's rows, in row order.
+ * Results are the same from one call to the next.
+ */
+size_t libra_attn_window_workspace_size(int64_t num_tiles, int64_t num_samples, int64_t n_q_rows,
+                                        int64_t n_kv_rows, int32_t h_q, int32_t h_kv,
+                                        int32_t head_dim, int64_t window, int64_t sinks,
+                                        int32_t backward);
+int libra_attn_window_fwd(const void *q, const void *k, const void *v, const int64_t *cu_seqlens,
+                          int64_t num_samples, const libra_tile_t *tiles, int64_t num_tiles,
+                          int64_t n_q_rows, int64_t n_kv_rows, int32_t h_q, int32_t h_kv,
+                          int32_t head_dim, int64_t window, int64_t sinks, float softmax_scale,
+                          void *o, float *lse, void *workspace, size_t workspace_bytes,
+                          void *stream);
+int libra_attn_window_bwd(const void *q, const void *k, const void *v, const void *o,
+                          const float *lse, const void *dout, const int64_t *cu_seqlens,
+                          int64_t num_samples, const libra_tile_t *tiles, int64_t num_tiles,
+                          int64_t n_q_rows, int64_t n_kv_rows, int32_t h_q, int32_t h_kv,
+                          int32_t head_dim, int64_t window, int64_t sinks, float softmax_scale,
+                          void *dq, void *dk, void *dv, uint32_t flags, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/*
+ * 8-bit activation checkpoints: what a layer's backward reads, held between
+ * the passes at 33/64 of bf16's bytes.  32 neighbouring elements of a row
+ * share a unit 2^e, the smallest power of two >= 2^-126 in which the largest
+ * of them rounds to at most 127; q holds the elements as integers,
+ * round(x / unit) with ties to even, and the byte e holds the exponent + 127,
+ * or 255 for a group with an infinity or a NaN (read back as 32 NaN).  Half a
+ * unit is at most 2^-7 of the group's largest element (of 2^-126 * 64, if that
+ * is more).  Units end at 2^121: larger magnitudes than 127 of it become 127.  Held values are exact
+ * in bf16 and fp32: packing them again gives the same values.
+ *   x [rows][cols]: device, LIBRA_BF16 or LIBRA_FP32 (else EUNSUPPORTED), rows
+ *       ld elements apart (ld >= cols), 16-byte aligned, ld whole 16 bytes.
+ *   q [rows][cols] int8 (16-byte aligned), e [rows][cols / 32] uint8: device,
+ *       contiguous.  cols is a multiple of 32.
+ * rows = 0 or cols = 0 does nothing.  Errors: EINVAL, EUNSUPPORTED, EOVERFLOW
+ * (rows * ld), EHIP.
+ */
+#define LIBRA_BF16 0
+#define LIBRA_FP32 1
+int libra_ckpt8_pack(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ld,
+                     int8_t *q, uint8_t *e, void *stream);
+int libra_ckpt8_unpack(const int8_t *q, const uint8_t *e, int64_t rows, int64_t cols,
+                       int32_t dtype, int64_t ld, void *x, void *stream);
+
+/* One held tensor (device pointers; the struct itself is read on the host during the call). */
+typedef struct libra_ckpt8 {
+  const int8_t *q;
+  const uint8_t *e;
+} libra_ckpt8_t;
+
+/*
+ * libra_attn_bwd_ckpt8 -- libra_attn_bwd (window = sinks = 0) or
+ * libra_attn_window_bwd (window >= 1) with q, k, v and o held in 8 bits, laid
+ * out as the tensors are.  The gradients are those of the formulas with the
+ * held values, lse and dout as given: P = exp(q K^T * scale - LSE) and
+ * D = rowsum(dO * O), for dQ and for dK alike (libra_attn_bwd, whose O and LSE
+ * belong to its q, k and v, corrects D by the sums of dS; here the rows of P
+ * need not sum to 1).
+ *   lse: fp32, of the forward on the values before packing.
+ *   workspace: >= libra_attn_bwd_ckpt8_workspace_size bytes, 256-byte aligned
+ *       (the unpacked tensors, then a backward's workspace).
+ * Everything else as in libra_attn_bwd.
+ */
+size_t libra_attn_bwd_ckpt8_workspace_size(int64_t num_tiles, int64_t num_samples,
+                                           int64_t n_q_rows, int64_t n_kv_rows, int32_t h_q,
+                                           int32_t h_kv, int32_t head_dim, int64_t window,
+                                           int64_t sinks);
+int libra_attn_bwd_ckpt8(const libra_ckpt8_t *q, const libra_ckpt8_t *k, const libra_ckpt8_t *v,
+                         const libra_ckpt8_t *o, const float *lse, const void *dout,
+                         const int64_t *cu_seqlens, int64_t num_samples,
+                         const libra_tile_t *tiles, int64_t num_tiles, int64_t n_q_rows,
+                         int64_t n_kv_rows, int32_t h_q, int32_t h_kv, int32_t head_dim,
+                         int64_t window, int64_t sinks, float softmax_scale, void *dq, void *dk,
+                         void *dv, uint32_t flags, void *workspace, size_t workspace_bytes,
+                         void *stream);
+
+/*
  * Kernel timing (tracing aid).  libra_timing_enable(1) clears the records of
  * the calling thread and makes every later libra_attn_fwd / libra_attn_bwd
- * call on that thread record HIP events on its stream around its main
+ * call (windowed and checkpoint ones too) on that thread record HIP events on its stream around its main
  * persistent kernels (the work-item kernels, not the small preparation
  * passes); libra_timing_enable(0) stops recording.  libra_timing_read waits
  * for the recorded events and returns the summed milliseconds and the number

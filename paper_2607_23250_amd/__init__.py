@@ -36,7 +36,12 @@ assert TILE_DTYPE.itemsize == 56
 EXPORTED = ("libra_strerror", "libra_last_error", "libra_plan", "libra_vrsp",
             "libra_attn_workspace_size", "libra_attn_fwd", "libra_attn_bwd",
             "libra_timing_enable", "libra_timing_read", "libra_mfma_loop_size",
-            "libra_mfma_loop", "libra_attn_skipped_tiles", "libra_attn_fwd_noalloc")
+            "libra_mfma_loop", "libra_attn_skipped_tiles", "libra_attn_fwd_noalloc",
+            "libra_attn_window_workspace_size", "libra_attn_window_fwd",
+            "libra_attn_window_bwd", "libra_ckpt8_pack", "libra_ckpt8_unpack",
+            "libra_attn_bwd_ckpt8_workspace_size", "libra_attn_bwd_ckpt8")
+LIBRA_BF16 = 0
+LIBRA_FP32 = 1
 LIBRA_WS_SKIPPED_OFFSET = 16
 LIBRA_FWD_NOALLOC_MAX_WORKSPACE = 16 << 20
 
@@ -51,6 +56,10 @@ class _PlanCfg(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "block_tokens", "head_shards", "num_packs", "cp", "num_q_heads", "num_kv_heads",
         "head_dim", "elem_bytes", "tau_num", "tau_den")]
+
+
+class _Ckpt8(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("e", ctypes.c_void_p)]
 
 
 _lib = None
@@ -97,6 +106,26 @@ def lib() -> ctypes.CDLL:
                                          ctypes.c_float, P, P, P]
     L.libra_attn_skipped_tiles.restype = ctypes.c_int
     L.libra_attn_skipped_tiles.argtypes = [P, ctypes.POINTER(ctypes.c_int32), P]
+    L.libra_attn_window_workspace_size.restype = SZ
+    L.libra_attn_window_workspace_size.argtypes = [I64, I64, I64, I64, I32, I32, I32, I64, I64, I32]
+    L.libra_attn_window_fwd.restype = ctypes.c_int
+    L.libra_attn_window_fwd.argtypes = [P, P, P, P, I64, P, I64, I64, I64, I32, I32, I32, I64, I64,
+                                        ctypes.c_float, P, P, P, SZ, P]
+    L.libra_attn_window_bwd.restype = ctypes.c_int
+    L.libra_attn_window_bwd.argtypes = [P, P, P, P, P, P, P, I64, P, I64, I64, I64, I32, I32, I32,
+                                        I64, I64, ctypes.c_float, P, P, P, ctypes.c_uint32, P, SZ,
+                                        P]
+    L.libra_ckpt8_pack.restype = ctypes.c_int
+    L.libra_ckpt8_pack.argtypes = [P, I32, I64, I64, I64, P, P, P]
+    L.libra_ckpt8_unpack.restype = ctypes.c_int
+    L.libra_ckpt8_unpack.argtypes = [P, P, I64, I64, I32, I64, P, P]
+    L.libra_attn_bwd_ckpt8_workspace_size.restype = SZ
+    L.libra_attn_bwd_ckpt8_workspace_size.argtypes = [I64, I64, I64, I64, I32, I32, I32, I64, I64]
+    C8 = ctypes.POINTER(_Ckpt8)
+    L.libra_attn_bwd_ckpt8.restype = ctypes.c_int
+    L.libra_attn_bwd_ckpt8.argtypes = [C8, C8, C8, C8, P, P, P, I64, P, I64, I64, I64, I32, I32,
+                                       I32, I64, I64, ctypes.c_float, P, P, P, ctypes.c_uint32, P,
+                                       SZ, P]
     _lib = L
     return L
 
@@ -353,4 +382,238 @@ def libra_attn_bwd(q, k, v, o, lse, dout, cu_seqlens, tiles, *, softmax_scale: f
                                 LIBRA_BWD_ACCUMULATE_DKV if accumulate else 0,
                                 workspace.data_ptr(), workspace.numel(), _stream(q.device)),
            "libra_attn_bwd")
+    return dq, dk, dv
+
+
+# ---------------------------------------------------------------------------
+# windowed attention and 8-bit checkpoints
+
+def _same_device(ref, *named):
+    """Every tensor on the device of ``ref`` (the call runs on that device's
+    current stream, whichever device is current)."""
+    for t, name in named:
+        if t is not None and t.device != ref.device:
+            raise ValueError(f"{name}: on {t.device}, the call runs on {ref.device}")
+
+
+def _attn_sizes(q, k, cu_seqlens, tiles):
+    if len(q.shape) != 3 or len(k.shape) != 3:
+        raise ValueError("q and k: need [rows][heads][head_dim]")
+    if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
+        raise ValueError("cu_seqlens: need num_samples + 1 offsets")
+    torch = _torch()
+    if tiles.dtype != torch.uint8 or not tiles.is_cuda or not tiles.is_contiguous() \
+            or tiles.numel() % TILE_DTYPE.itemsize:
+        raise ValueError("tiles: need a device tensor from tiles_to_device")
+    n_q, h_q, d = q.shape
+    n_kv, h_kv, _ = k.shape
+    return (tiles.numel() // TILE_DTYPE.itemsize, cu_seqlens.numel() - 1, n_q, n_kv, h_q, h_kv, d)
+
+
+def _workspace(workspace, need, device):
+    torch = _torch()
+    if workspace is None:
+        return alloc_workspace(need, device)
+    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace: need a contiguous uint8 tensor (alloc_workspace)")
+    return workspace
+
+
+def libra_attn_window_workspace_size(num_tiles: int, num_samples: int, n_q_rows: int,
+                                     n_kv_rows: int, h_q: int, h_kv: int, head_dim: int,
+                                     backward: bool, *, window: int, sinks: int = 0) -> int:
+    return int(lib().libra_attn_window_workspace_size(
+        num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, window, sinks,
+        int(bool(backward))))
+
+
+def libra_attn_window_fwd(q, k, v, cu_seqlens, tiles, *, window: int, sinks: int = 0,
+                          softmax_scale: float = 0.0, o=None, lse=None, workspace=None):
+    """``libra_attn_fwd`` in which the row at position p of a sample attends the
+    keys ``p - window + 1 .. p`` and the sample's first ``sinks`` keys."""
+    torch = _torch()
+    sizes = _attn_sizes(q, k, cu_seqlens, tiles)
+    T, n, n_q, n_kv, h_q, h_kv, d = sizes
+    _need(q, torch.bfloat16, (n_q, h_q, d), "q")
+    _need(k, torch.bfloat16, (n_kv, h_kv, d), "k")
+    _need(v, torch.bfloat16, (n_kv, h_kv, d), "v")
+    _need(cu_seqlens, torch.int64, (n + 1,), "cu_seqlens")
+    _same_device(q, (k, "k"), (v, "v"), (cu_seqlens, "cu_seqlens"), (tiles, "tiles"), (o, "o"),
+                 (lse, "lse"), (workspace, "workspace"))
+    if o is None:
+        o = torch.empty_like(q)
+    if lse is None:
+        lse = torch.empty((h_q, n_q), dtype=torch.float32, device=q.device)
+    _need(o, torch.bfloat16, (n_q, h_q, d), "o")
+    _need(lse, torch.float32, (h_q, n_q), "lse")
+    workspace = _workspace(workspace, 0 if workspace is not None else
+                           libra_attn_window_workspace_size(*sizes, False, window=window,
+                                                            sinks=sinks), q.device)
+    with torch.cuda.device(q.device):
+        _check(lib().libra_attn_window_fwd(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_seqlens.data_ptr(), n, tiles.data_ptr(),
+            T, n_q, n_kv, h_q, h_kv, d, window, sinks, softmax_scale, o.data_ptr(),
+            lse.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(q.device)),
+            "libra_attn_window_fwd")
+    return o, lse
+
+
+def _grad_buffers(like_q, k_shape, accumulate, dq, dk, dv):
+    """(dq, dk, dv), made where they are not given, checked where they are."""
+    torch = _torch()
+    kv_dtype = torch.float32 if accumulate else torch.bfloat16
+    if dq is None:
+        dq = torch.empty_like(like_q)
+    make = torch.zeros if accumulate else torch.empty
+    if dk is None:
+        dk = make(k_shape, dtype=kv_dtype, device=like_q.device)
+    if dv is None:
+        dv = make(k_shape, dtype=kv_dtype, device=like_q.device)
+    _need(dq, torch.bfloat16, like_q.shape, "dq")
+    _need(dk, kv_dtype, k_shape, "dk")
+    _need(dv, kv_dtype, k_shape, "dv")
+    return dq, dk, dv
+
+
+def libra_attn_window_bwd(q, k, v, o, lse, dout, cu_seqlens, tiles, *, window: int,
+                          sinks: int = 0, softmax_scale: float = 0.0, dq=None, dk=None, dv=None,
+                          accumulate: bool = False, workspace=None):
+    """Gradients of ``libra_attn_window_fwd``: dQ (bf16), dK / dV (bf16, or fp32
+    summed into when ``accumulate``)."""
+    torch = _torch()
+    sizes = _attn_sizes(q, k, cu_seqlens, tiles)
+    T, n, n_q, n_kv, h_q, h_kv, d = sizes
+    for t, name in ((q, "q"), (o, "o"), (dout, "dout")):
+        _need(t, torch.bfloat16, (n_q, h_q, d), name)
+    for t, name in ((k, "k"), (v, "v")):
+        _need(t, torch.bfloat16, (n_kv, h_kv, d), name)
+    _need(lse, torch.float32, (h_q, n_q), "lse")
+    _need(cu_seqlens, torch.int64, (n + 1,), "cu_seqlens")
+    _same_device(q, (k, "k"), (v, "v"), (o, "o"), (lse, "lse"), (dout, "dout"),
+                 (cu_seqlens, "cu_seqlens"), (tiles, "tiles"), (dq, "dq"), (dk, "dk"),
+                 (dv, "dv"), (workspace, "workspace"))
+    dq, dk, dv = _grad_buffers(q, (n_kv, h_kv, d), accumulate, dq, dk, dv)
+    workspace = _workspace(workspace, 0 if workspace is not None else
+                           libra_attn_window_workspace_size(*sizes, True, window=window,
+                                                            sinks=sinks), q.device)
+    with torch.cuda.device(q.device):
+        _check(lib().libra_attn_window_bwd(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+            dout.data_ptr(), cu_seqlens.data_ptr(), n, tiles.data_ptr(), T, n_q, n_kv, h_q, h_kv,
+            d, window, sinks, softmax_scale, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+            LIBRA_BWD_ACCUMULATE_DKV if accumulate else 0, workspace.data_ptr(),
+            workspace.numel(), _stream(q.device)), "libra_attn_window_bwd")
+    return dq, dk, dv
+
+
+def _rows_cols_ld(x, name):
+    """(rows, cols, ld) of a tensor whose last axis is dense and whose other axes
+    are one row index at a fixed stride."""
+    cols = x.shape[-1]
+    rows = x.numel() // cols if cols else 0
+    if rows == 0 or x.is_contiguous():
+        return rows, cols, cols
+    if x.stride(-1) != 1 and cols > 1:
+        raise ValueError(f"{name}: the last axis must be dense")
+    # axes of one element have any stride
+    lead = [(n, s) for n, s in zip(x.shape[:-1], x.stride()[:-1]) if n > 1]
+    for (_, s0), (n1, s1) in zip(lead, lead[1:]):
+        if s0 != n1 * s1:
+            raise ValueError(f"{name}: the leading axes must lie at one stride")
+    return rows, cols, (lead[-1][1] if lead else cols)
+
+
+def _ckpt8_type(dtype, name):
+    torch = _torch()
+    types = {torch.bfloat16: LIBRA_BF16, torch.float32: LIBRA_FP32}
+    if dtype not in types:
+        raise ValueError(f"{name}: need torch.bfloat16 or torch.float32, got {dtype}")
+    return types[dtype]
+
+
+def libra_ckpt8_pack(x, *, q=None, e=None):
+    """Holds ``x`` ([..., cols], bf16 or fp32, cols a multiple of 32) in 8 bits:
+    ``(q, e)``, int8 of x's shape and uint8 exponents [..., cols / 32].  The
+    leading axes of ``x`` may lie at a larger stride (a slice of a wider tensor)."""
+    torch = _torch()
+    if not x.is_cuda or x.dim() < 1:
+        raise ValueError("x: need a device tensor of one axis or more")
+    dtype = _ckpt8_type(x.dtype, "x")
+    if x.shape[-1] % 32:
+        raise ValueError(f"x: the last axis ({x.shape[-1]}) must be a multiple of 32")
+    rows, cols, ld = _rows_cols_ld(x, "x")
+    e_shape = (*x.shape[:-1], cols // 32)
+    if q is None:
+        q = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    if e is None:
+        e = torch.empty(e_shape, dtype=torch.uint8, device=x.device)
+    _need(q, torch.int8, x.shape, "q")
+    _need(e, torch.uint8, e_shape, "e")
+    _same_device(x, (q, "q"), (e, "e"))
+    with torch.cuda.device(x.device):
+        _check(lib().libra_ckpt8_pack(x.data_ptr(), dtype, rows, cols, ld, q.data_ptr(),
+                                      e.data_ptr(), _stream(x.device)), "libra_ckpt8_pack")
+    return q, e
+
+
+def libra_ckpt8_unpack(q, e, *, dtype=None, out=None):
+    """The values that ``libra_ckpt8_pack`` holds, as ``dtype`` (bf16, or torch.float32),
+    or in ``out`` (whose leading axes may lie at a larger stride)."""
+    torch = _torch()
+    if q.dim() < 1 or q.shape[-1] % 32:
+        raise ValueError("q: the last axis must be a multiple of 32")
+    _need(q, torch.int8, q.shape, "q")
+    _need(e, torch.uint8, (*q.shape[:-1], q.shape[-1] // 32), "e")
+    if out is None:
+        out = torch.empty(q.shape, dtype=dtype or torch.bfloat16, device=q.device)
+    elif dtype is not None and out.dtype != dtype:
+        raise ValueError(f"out: {out.dtype}, dtype asks for {dtype}")
+    kind = _ckpt8_type(out.dtype, "out")
+    if out.shape != q.shape:
+        raise ValueError(f"out: need shape {tuple(q.shape)}, got {tuple(out.shape)}")
+    _same_device(q, (e, "e"), (out, "out"))
+    rows, cols, ld = _rows_cols_ld(out, "out")
+    with torch.cuda.device(q.device):
+        _check(lib().libra_ckpt8_unpack(q.data_ptr(), e.data_ptr(), rows, cols, kind, ld,
+                                        out.data_ptr(), _stream(q.device)), "libra_ckpt8_unpack")
+    return out
+
+
+def libra_attn_bwd_ckpt8_workspace_size(num_tiles: int, num_samples: int, n_q_rows: int,
+                                        n_kv_rows: int, h_q: int, h_kv: int, head_dim: int, *,
+                                        window: int = 0, sinks: int = 0) -> int:
+    return int(lib().libra_attn_bwd_ckpt8_workspace_size(
+        num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, window, sinks))
+
+
+def libra_attn_bwd_ckpt8(q, k, v, o, lse, dout, cu_seqlens, tiles, *, window: int = 0,
+                         sinks: int = 0, softmax_scale: float = 0.0, dq=None, dk=None, dv=None,
+                         accumulate: bool = False, workspace=None):
+    """``libra_attn_bwd`` (``window`` 0) or ``libra_attn_window_bwd`` from ``q``, ``k``,
+    ``v`` and ``o`` as ``libra_ckpt8_pack`` holds them: pairs ``(q, e)``."""
+    torch = _torch()
+    sizes = _attn_sizes(q[0], k[0], cu_seqlens, tiles)
+    T, n, n_q, n_kv, h_q, h_kv, d = sizes
+    held, shapes = (q, k, v, o), ((n_q, h_q, d), (n_kv, h_kv, d), (n_kv, h_kv, d), (n_q, h_q, d))
+    ref = q[0]
+    for (x, e), shape, name in zip(held, shapes, "qkvo"):
+        _need(x, torch.int8, shape, f"{name}[0]")
+        _need(e, torch.uint8, (*shape[:2], d // 32), f"{name}[1]")
+        _same_device(ref, (x, f"{name}[0]"), (e, f"{name}[1]"))
+    _need(dout, torch.bfloat16, (n_q, h_q, d), "dout")
+    _need(lse, torch.float32, (h_q, n_q), "lse")
+    _need(cu_seqlens, torch.int64, (n + 1,), "cu_seqlens")
+    _same_device(ref, (lse, "lse"), (dout, "dout"), (cu_seqlens, "cu_seqlens"), (tiles, "tiles"),
+                 (dq, "dq"), (dk, "dk"), (dv, "dv"), (workspace, "workspace"))
+    dq, dk, dv = _grad_buffers(dout, (n_kv, h_kv, d), accumulate, dq, dk, dv)
+    workspace = _workspace(workspace, 0 if workspace is not None else
+                           libra_attn_bwd_ckpt8_workspace_size(*sizes, window=window,
+                                                               sinks=sinks), ref.device)
+    c = [ctypes.byref(_Ckpt8(x.data_ptr(), e.data_ptr())) for x, e in held]
+    with torch.cuda.device(ref.device):
+        _check(lib().libra_attn_bwd_ckpt8(
+            *c, lse.data_ptr(), dout.data_ptr(), cu_seqlens.data_ptr(), n, tiles.data_ptr(), T,
+            n_q, n_kv, h_q, h_kv, d, window, sinks, softmax_scale, dq.data_ptr(), dk.data_ptr(),
+            dv.data_ptr(), LIBRA_BWD_ACCUMULATE_DKV if accumulate else 0, workspace.data_ptr(),
+            workspace.numel(), _stream(ref.device)), "libra_attn_bwd_ckpt8")
     return dq, dk, dv

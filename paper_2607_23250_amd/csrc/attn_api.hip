@@ -8,6 +8,8 @@
 #include <vector>
 
 #include "attn_common.h"
+#include "attn_win_items.h"
+#include "ckpt8.h"
 #include "errors.h"
 #include "libra.h"
 
@@ -65,6 +67,17 @@ int check_ws(const void *ws, size_t bytes, size_t need) {
     return fail(LIBRA_EINVAL, "workspace must be 256-byte aligned");
   if (bytes < need)
     return fail(LIBRA_ENOSPC, "workspace of %zu bytes, need %zu", bytes, need);
+  return LIBRA_OK;
+}
+
+// The window and sinks of a call, clamped to what the rows can reach.
+int check_window(int64_t window, int64_t sinks, int64_t n_kv, Window *out) {
+  if (window < 1) return fail(LIBRA_EINVAL, "window must be >= 1 (got %lld)", (long long)window);
+  if (sinks < 0) return fail(LIBRA_EINVAL, "sinks must be >= 0 (got %lld)", (long long)sinks);
+  if (sinks > kMaxSinks)
+    return fail(LIBRA_EUNSUPPORTED, "%lld sinks (at most %d)", (long long)sinks, kMaxSinks);
+  out->size = (int32_t)(window < n_kv ? window : n_kv);
+  out->sinks = (int32_t)(sinks < n_kv ? sinks : n_kv);
   return LIBRA_OK;
 }
 
@@ -135,14 +148,14 @@ extern "C" size_t libra_attn_workspace_size(int64_t num_tiles, int64_t num_sampl
   return fwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim).total;
 }
 
-extern "C" int libra_attn_fwd(const void *q, const void *k, const void *v,
-                              const int64_t *cu_seqlens, int64_t num_samples,
-                              const libra_tile_t *tiles, int64_t num_tiles, int64_t n_q_rows,
-                              int64_t n_kv_rows, int32_t h_q, int32_t h_kv, int32_t head_dim,
-                              float softmax_scale, void *o, float *lse, void *workspace,
-                              size_t workspace_bytes, void *stream) {
-  last_error_text().clear();
-  if (int rc = check_sizes(num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim)) return rc;
+namespace {
+
+// libra_attn_fwd, or with a window libra_attn_window_fwd, after the window's checks.
+int attn_fwd(const void *q, const void *k, const void *v, const int64_t *cu_seqlens,
+             int64_t num_samples, const libra_tile_t *tiles, int64_t num_tiles, int64_t n_q_rows,
+             int64_t n_kv_rows, int32_t h_q, int32_t h_kv, int32_t head_dim, float softmax_scale,
+             void *o, float *lse, void *workspace, size_t workspace_bytes, void *stream,
+             const Window &win) {
   if (num_tiles < 0) return fail(LIBRA_EINVAL, "num_tiles < 0");
   if (num_tiles == 0) return LIBRA_OK;
   if (!q || !k || !v || !cu_seqlens || !tiles || !o || !lse)
@@ -156,7 +169,81 @@ extern "C" int libra_attn_fwd(const void *q, const void *k, const void *v,
   if (rc) return rc;
   return launch_fwd(q, k, v, cu_seqlens, num_samples, tiles, num_tiles, n_q_rows, n_kv_rows, h_q,
                     h_kv, head_dim, scale, o, lse, workspace, L,
-                    static_cast<hipStream_t>(stream), tm);
+                    static_cast<hipStream_t>(stream), tm, win);
+}
+
+// The checks of a backward call that come before its workspace's.
+int check_bwd(const void *q, const void *k, const void *v, const void *o, const float *lse,
+              const void *dout, const int64_t *cu_seqlens, const libra_tile_t *tiles,
+              int64_t num_tiles, const void *dq, const void *dk, const void *dv, uint32_t flags) {
+  if (num_tiles < 0) return fail(LIBRA_EINVAL, "num_tiles < 0");
+  if (flags & ~LIBRA_BWD_ACCUMULATE_DKV) return fail(LIBRA_EINVAL, "unknown flags 0x%x", flags);
+  if (!dk || !dv) return fail(LIBRA_EINVAL, "NULL dk / dv");
+  if (num_tiles > 0 && (!q || !k || !v || !o || !lse || !dout || !cu_seqlens || !tiles || !dq))
+    return fail(LIBRA_EINVAL, "NULL tensor argument");
+  return LIBRA_OK;
+}
+
+// A backward after its checks.
+int attn_bwd(const void *q, const void *k, const void *v, const void *o, const float *lse,
+             const void *dout, const int64_t *cu_seqlens, int64_t num_samples,
+             const libra_tile_t *tiles, int64_t num_tiles, int64_t n_q_rows, int64_t n_kv_rows,
+             int32_t h_q, int32_t h_kv, int32_t head_dim, float softmax_scale, void *dq, void *dk,
+             void *dv, uint32_t flags, void *workspace, const BwdLayout &L, void *stream,
+             bool exact_o, const Window &win) {
+  const float scale = softmax_scale > 0.f ? softmax_scale : 1.f / std::sqrt((float)head_dim);
+  int rc = LIBRA_OK;
+  const KernelTimer *tm_kv = num_tiles > 0 ? next_timer(1, &rc) : nullptr;
+  if (rc) return rc;
+  const KernelTimer *tm_q = num_tiles > 0 ? next_timer(2, &rc) : nullptr;
+  if (rc) return rc;
+  return launch_bwd(q, k, v, o, lse, dout, cu_seqlens, num_samples, tiles, num_tiles, n_q_rows,
+                    n_kv_rows, h_q, h_kv, head_dim, scale, dq, dk, dv,
+                    (flags & LIBRA_BWD_ACCUMULATE_DKV) != 0, workspace, L,
+                    static_cast<hipStream_t>(stream), tm_kv, tm_q, exact_o, win);
+}
+
+}  // namespace
+
+extern "C" int libra_attn_fwd(const void *q, const void *k, const void *v,
+                              const int64_t *cu_seqlens, int64_t num_samples,
+                              const libra_tile_t *tiles, int64_t num_tiles, int64_t n_q_rows,
+                              int64_t n_kv_rows, int32_t h_q, int32_t h_kv, int32_t head_dim,
+                              float softmax_scale, void *o, float *lse, void *workspace,
+                              size_t workspace_bytes, void *stream) {
+  last_error_text().clear();
+  if (int rc = check_sizes(num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim)) return rc;
+  return attn_fwd(q, k, v, cu_seqlens, num_samples, tiles, num_tiles, n_q_rows, n_kv_rows, h_q,
+                  h_kv, head_dim, softmax_scale, o, lse, workspace, workspace_bytes, stream, {});
+}
+
+extern "C" size_t libra_attn_window_workspace_size(int64_t num_tiles, int64_t num_samples,
+                                                   int64_t n_q_rows, int64_t n_kv_rows,
+                                                   int32_t h_q, int32_t h_kv, int32_t head_dim,
+                                                   int64_t window, int64_t sinks,
+                                                   int32_t backward) {
+  Window win;
+  if (num_tiles < 0 || check_sizes(num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim) ||
+      check_window(window, sinks, n_kv_rows, &win))
+    return 0;
+  if (backward)
+    return bwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, win).total;
+  return fwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim).total;
+}
+
+extern "C" int libra_attn_window_fwd(const void *q, const void *k, const void *v,
+                                     const int64_t *cu_seqlens, int64_t num_samples,
+                                     const libra_tile_t *tiles, int64_t num_tiles,
+                                     int64_t n_q_rows, int64_t n_kv_rows, int32_t h_q,
+                                     int32_t h_kv, int32_t head_dim, int64_t window,
+                                     int64_t sinks, float softmax_scale, void *o, float *lse,
+                                     void *workspace, size_t workspace_bytes, void *stream) {
+  last_error_text().clear();
+  Window win;
+  if (int rc = check_sizes(num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim)) return rc;
+  if (int rc = check_window(window, sinks, n_kv_rows, &win)) return rc;
+  return attn_fwd(q, k, v, cu_seqlens, num_samples, tiles, num_tiles, n_q_rows, n_kv_rows, h_q,
+                  h_kv, head_dim, softmax_scale, o, lse, workspace, workspace_bytes, stream, win);
 }
 
 extern "C" int libra_attn_fwd_noalloc(const void *q, const void *k, const void *v,
@@ -210,23 +297,154 @@ extern "C" int libra_attn_bwd(const void *q, const void *k, const void *v, const
                               void *stream) {
   last_error_text().clear();
   if (int rc = check_sizes(num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim)) return rc;
-  if (num_tiles < 0) return fail(LIBRA_EINVAL, "num_tiles < 0");
-  if (flags & ~LIBRA_BWD_ACCUMULATE_DKV) return fail(LIBRA_EINVAL, "unknown flags 0x%x", flags);
-  if (!dk || !dv) return fail(LIBRA_EINVAL, "NULL dk / dv");
-  if (num_tiles > 0 && (!q || !k || !v || !o || !lse || !dout || !cu_seqlens || !tiles || !dq))
-    return fail(LIBRA_EINVAL, "NULL tensor argument");
+  if (int rc = check_bwd(q, k, v, o, lse, dout, cu_seqlens, tiles, num_tiles, dq, dk, dv, flags))
+    return rc;
   const BwdLayout L =
       bwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim);
   if (num_tiles > 0)
     if (int rc = check_ws(workspace, workspace_bytes, L.total)) return rc;
-  const float scale = softmax_scale > 0.f ? softmax_scale : 1.f / std::sqrt((float)head_dim);
-  int rc = LIBRA_OK;
-  const KernelTimer *tm_kv = num_tiles > 0 ? next_timer(1, &rc) : nullptr;
-  if (rc) return rc;
-  const KernelTimer *tm_q = num_tiles > 0 ? next_timer(2, &rc) : nullptr;
-  if (rc) return rc;
-  return launch_bwd(q, k, v, o, lse, dout, cu_seqlens, num_samples, tiles, num_tiles, n_q_rows,
-                    n_kv_rows, h_q, h_kv, head_dim, scale, dq, dk, dv,
-                    (flags & LIBRA_BWD_ACCUMULATE_DKV) != 0, workspace, L,
-                    static_cast<hipStream_t>(stream), tm_kv, tm_q);
+  return attn_bwd(q, k, v, o, lse, dout, cu_seqlens, num_samples, tiles, num_tiles, n_q_rows,
+                  n_kv_rows, h_q, h_kv, head_dim, softmax_scale, dq, dk, dv, flags, workspace, L,
+                  stream, true, {});
+}
+
+extern "C" int libra_attn_window_bwd(const void *q, const void *k, const void *v, const void *o,
+                                     const float *lse, const void *dout,
+                                     const int64_t *cu_seqlens, int64_t num_samples,
+                                     const libra_tile_t *tiles, int64_t num_tiles,
+                                     int64_t n_q_rows, int64_t n_kv_rows, int32_t h_q,
+                                     int32_t h_kv, int32_t head_dim, int64_t window,
+                                     int64_t sinks, float softmax_scale, void *dq, void *dk,
+                                     void *dv, uint32_t flags, void *workspace,
+                                     size_t workspace_bytes, void *stream) {
+  last_error_text().clear();
+  Window win;
+  if (int rc = check_sizes(num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim)) return rc;
+  if (int rc = check_window(window, sinks, n_kv_rows, &win)) return rc;
+  if (int rc = check_bwd(q, k, v, o, lse, dout, cu_seqlens, tiles, num_tiles, dq, dk, dv, flags))
+    return rc;
+  const BwdLayout L =
+      bwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, win);
+  if (num_tiles > 0)
+    if (int rc = check_ws(workspace, workspace_bytes, L.total)) return rc;
+  return attn_bwd(q, k, v, o, lse, dout, cu_seqlens, num_samples, tiles, num_tiles, n_q_rows,
+                  n_kv_rows, h_q, h_kv, head_dim, softmax_scale, dq, dk, dv, flags, workspace, L,
+                  stream, true, win);
+}
+
+// ---------------------------------------------------------------------------
+// 8-bit checkpoints.
+namespace {
+
+int check_ckpt8(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ld,
+                const void *q, const void *e) {
+  if (dtype != LIBRA_BF16 && dtype != LIBRA_FP32)
+    return fail(LIBRA_EUNSUPPORTED, "dtype %d (supported: LIBRA_BF16, LIBRA_FP32)", dtype);
+  if (rows < 0 || cols < 0 || cols % 32)
+    return fail(LIBRA_EINVAL, "need rows >= 0 and cols a multiple of 32 (got %lld x %lld)",
+                (long long)rows, (long long)cols);
+  const int64_t align = dtype == LIBRA_BF16 ? 8 : 4;   // elements of 16 bytes
+  if (ld < cols || ld % align)
+    return fail(LIBRA_EINVAL, "ld must be >= cols and a multiple of %lld (got %lld)",
+                (long long)align, (long long)ld);
+  if (rows && ld > (INT64_MAX >> 4) / rows) return fail(LIBRA_EOVERFLOW, "rows * ld overflows");
+  if (rows && cols) {
+    if (!x || !q || !e) return fail(LIBRA_EINVAL, "NULL tensor argument");
+    if (reinterpret_cast<uintptr_t>(x) % 16 || reinterpret_cast<uintptr_t>(q) % 16)
+      return fail(LIBRA_EINVAL, "x and q must be 16-byte aligned");
+  }
+  return LIBRA_OK;
+}
+
+// Workspace of libra_attn_bwd_ckpt8: the unpacked q, k, v, o, then a backward's.
+struct Ckpt8Layout {
+  size_t at[4], bwd = 0, total = 0;
+  BwdLayout L;
+};
+size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+Ckpt8Layout ckpt8_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d,
+                         const Window &win) {
+  Ckpt8Layout c;
+  c.L = bwd_layout(T, n, n_q, n_kv, h_q, h_kv, d, win);
+  const size_t q = align256((size_t)n_q * h_q * d * 2), k = align256((size_t)n_kv * h_kv * d * 2);
+  c.at[0] = 0;
+  c.at[1] = q;
+  c.at[2] = q + k;
+  c.at[3] = q + 2 * k;
+  c.bwd = 2 * q + 2 * k;
+  c.total = c.bwd + c.L.total;
+  return c;
+}
+
+}  // namespace
+
+extern "C" int libra_ckpt8_pack(const void *x, int32_t dtype, int64_t rows, int64_t cols,
+                                int64_t ld, int8_t *q, uint8_t *e, void *stream) {
+  last_error_text().clear();
+  if (int rc = check_ckpt8(x, dtype, rows, cols, ld, q, e)) return rc;
+  if (rows == 0 || cols == 0) return LIBRA_OK;
+  return launch_ckpt8_pack(x, dtype == LIBRA_FP32, rows, cols, ld, q, e,
+                           static_cast<hipStream_t>(stream));
+}
+
+extern "C" int libra_ckpt8_unpack(const int8_t *q, const uint8_t *e, int64_t rows, int64_t cols,
+                                  int32_t dtype, int64_t ld, void *x, void *stream) {
+  last_error_text().clear();
+  if (int rc = check_ckpt8(x, dtype, rows, cols, ld, q, e)) return rc;
+  if (rows == 0 || cols == 0) return LIBRA_OK;
+  return launch_ckpt8_unpack(q, e, rows, cols, dtype == LIBRA_FP32, ld, x,
+                             static_cast<hipStream_t>(stream));
+}
+
+extern "C" size_t libra_attn_bwd_ckpt8_workspace_size(int64_t num_tiles, int64_t num_samples,
+                                                      int64_t n_q_rows, int64_t n_kv_rows,
+                                                      int32_t h_q, int32_t h_kv,
+                                                      int32_t head_dim, int64_t window,
+                                                      int64_t sinks) {
+  Window win;
+  if (num_tiles < 0 || check_sizes(num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim) ||
+      ((window || sinks) && check_window(window, sinks, n_kv_rows, &win)))
+    return 0;
+  return ckpt8_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, win).total;
+}
+
+extern "C" int libra_attn_bwd_ckpt8(const libra_ckpt8_t *q, const libra_ckpt8_t *k,
+                                    const libra_ckpt8_t *v, const libra_ckpt8_t *o,
+                                    const float *lse, const void *dout, const int64_t *cu_seqlens,
+                                    int64_t num_samples, const libra_tile_t *tiles,
+                                    int64_t num_tiles, int64_t n_q_rows, int64_t n_kv_rows,
+                                    int32_t h_q, int32_t h_kv, int32_t head_dim, int64_t window,
+                                    int64_t sinks, float softmax_scale, void *dq, void *dk,
+                                    void *dv, uint32_t flags, void *workspace,
+                                    size_t workspace_bytes, void *stream) {
+  last_error_text().clear();
+  Window win;
+  if (int rc = check_sizes(num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim)) return rc;
+  if (window || sinks)
+    if (int rc = check_window(window, sinks, n_kv_rows, &win)) return rc;
+  if (int rc = check_bwd(q, k, v, o, lse, dout, cu_seqlens, tiles, num_tiles, dq, dk, dv, flags))
+    return rc;
+  const Ckpt8Layout C =
+      ckpt8_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, win);
+  char *ws = static_cast<char *>(workspace);
+  if (num_tiles > 0) {
+    const libra_ckpt8_t *in[4] = {q, k, v, o};
+    Ckpt8Four four;
+    for (int i = 0; i < 4; ++i) {
+      const int64_t chunks = (i == 0 || i == 3 ? n_q_rows * h_q : n_kv_rows * h_kv) * head_dim / 16;
+      if (chunks && (!in[i]->q || !in[i]->e)) return fail(LIBRA_EINVAL, "NULL checkpoint pointer");
+      if (reinterpret_cast<uintptr_t>(in[i]->q) % 16)
+        return fail(LIBRA_EINVAL, "checkpoint integers must be 16-byte aligned");
+      four.q[i] = in[i]->q;
+      four.e[i] = in[i]->e;
+      four.x[i] = reinterpret_cast<bf16 *>(ws + C.at[i]);
+      four.chunks[i] = chunks;
+    }
+    if (int rc = check_ws(workspace, workspace_bytes, C.total)) return rc;
+    if (int rc = launch_ckpt8_unpack4(four, static_cast<hipStream_t>(stream))) return rc;
+  }
+  return attn_bwd(ws + C.at[0], ws + C.at[1], ws + C.at[2], ws + C.at[3], lse, dout, cu_seqlens,
+                  num_samples, tiles, num_tiles, n_q_rows, n_kv_rows, h_q, h_kv, head_dim,
+                  softmax_scale, dq, dk, dv, flags, num_tiles > 0 ? ws + C.bwd : ws, C.L, stream,
+                  false, win);
 }

@@ -40,25 +40,12 @@
 #include <cstdint>
 
 #include "attn_common.h"
+#include "attn_bwd_steps.h"
 #include "attn_items.h"
+#include "attn_win_items.h"
 #include "errors.h"
 
 namespace libra {
-
-__device__ __forceinline__ unsigned long long ld_agent(const unsigned long long *p) {
-  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
-// Bit set of the KV heads whose query groups intersect [hb, he); `odd` is set
-// if it covers an odd number of heads of one of them.
-__device__ __forceinline__ unsigned long long group_bits(int hb, int he, int G, bool &odd) {
-  unsigned long long m = 0;
-  for (int g = hb / G; g * G < he; ++g) {
-    m |= 1ull << g;
-    odd |= ((min(he, (g + 1) * G) - max(hb, g * G)) & 1) != 0;
-  }
-  return m;
-}
 
 // ---------------------------------------------------------------------------
 // One workgroup: per sample, the key extent attended by covered rows and the
@@ -544,13 +531,15 @@ __device__ __forceinline__ void absmax_q(unsigned block, const bf16 *__restrict_
 // its keys up to the end of the last 128-key block that those rows attend
 // (all KV heads).  One wave per key row.  CONVERT = false: max |K| and
 // max |V| over them; CONVERT = true: their scaled fp16 copies.
-template <int D, bool CONVERT>
+// WIN: `ext` holds WinSample records; keys that no covered row's window or sinks
+// reach, and keys past the last covered row, are left out.
+template <int D, bool CONVERT, bool WIN>
 __device__ __forceinline__ void kv_pass(unsigned block, unsigned blocks,
                                         const bf16 *__restrict__ k, const bf16 *__restrict__ v,
                                         const int64_t *__restrict__ cu, int64_t n,
                                         const int32_t *__restrict__ ext, int h_kv, int64_t n_kv,
                                         int32_t *__restrict__ hdr, f16 *__restrict__ k16,
-                                        f16 *__restrict__ v16) {
+                                        f16 *__restrict__ v16, const Window &win) {
   const int l = threadIdx.x & 63;
   const int64_t wave = ((int64_t)block * 256 + threadIdx.x) >> 6;
   const int64_t waves = (int64_t)blocks * 4;
@@ -561,16 +550,25 @@ __device__ __forceinline__ void kv_pass(unsigned block, unsigned blocks,
     s_v = fp16_scale((uint32_t)hdr[kMaxAbs + 3], true);
   }
   int64_t lo = 0, hi = 0, end = 0;   // rows [lo, hi) of the current sample; loaded keys end at `end`
+  int64_t from = 0, sink_end = 0;    // WIN: and start at `from`, but for those before sink_end
   for (int64_t row = wave; row < n_kv; row += waves) {
     if (row < lo || row >= hi) {
       const int64_t j = upper_bound64(cu, n, row) - 1;
       lo = cu[j];
       hi = cu[j + 1];
-      const int64_t e = (int64_t)ext[j];
-      const int64_t lim = (e + kBwdBK - 1) / kBwdBK * kBwdBK;
-      end = lo + (e > 0 ? (lim < hi - lo ? lim : hi - lo) : 0);
+      if constexpr (WIN) {
+        const WinSample &ws = reinterpret_cast<const WinSample *>(ext)[j];
+        end = lo + ws.ext;
+        from = lo + first_key_block(ws.beg, win) * kBwdBK;
+        sink_end = lo + (win.sinks + kBwdBK - 1) / kBwdBK * kBwdBK;
+      } else {
+        const int64_t e = (int64_t)ext[j];
+        const int64_t lim = (e + kBwdBK - 1) / kBwdBK * kBwdBK;
+        end = lo + (e > 0 ? (lim < hi - lo ? lim : hi - lo) : 0);
+      }
     }
     if (row >= end) continue;
+    if (WIN && row < from && row >= sink_end) continue;
     for (int c = l; c < chunks; c += 64) {
       const size_t off = (size_t)row * h_kv * D + 8 * (size_t)c;
       const bf16x8 kx = *reinterpret_cast<const bf16x8 *>(k + off);
@@ -698,14 +696,15 @@ struct BwdPass {
   uint4 *dk, *dv;                          // to be zeroed
   int64_t n16;                             // 16-byte pieces of each
   unsigned tile_blocks, kv_blocks, zero_blocks;
+  Window win;
 };
-template <int D>
+template <int D, bool WIN>
 __global__ __launch_bounds__(256) void bwd_max_kernel(BwdPass a) {
   unsigned b = blockIdx.x;
   if (b == 0 && threadIdx.x == 0 && a.hdr[kDqFull]) atomicAdd(&a.hdr[kBadTiles], 1);
   if (b < a.kv_blocks) {
-    kv_pass<D, false>(b, a.kv_blocks, a.k, a.v, a.cu, a.n, a.ext, a.h_kv, a.n_kv, a.hdr, a.k16,
-                      a.v16);
+    kv_pass<D, false, WIN>(b, a.kv_blocks, a.k, a.v, a.cu, a.n, a.ext, a.h_kv, a.n_kv, a.hdr,
+                           a.k16, a.v16, a.win);
   } else if ((b -= a.kv_blocks) < a.tile_blocks) {
     absmax_q<D>(b, a.q, a.dout, a.tiles, a.h_q, a.n_q, a.n_kv, a.cu[a.n], a.hdr, a.rec);
   } else {
@@ -714,12 +713,12 @@ __global__ __launch_bounds__(256) void bwd_max_kernel(BwdPass a) {
     zero_fill(b % half, half, b < half ? a.dk : a.dv, a.n16);
   }
 }
-template <int D>
+template <int D, bool WIN>
 __global__ __launch_bounds__(256) void bwd_copy_kernel(BwdPass a) {
   const unsigned b = blockIdx.x;
   if (b < a.kv_blocks)
-    kv_pass<D, true>(b, a.kv_blocks, a.k, a.v, a.cu, a.n, a.ext, a.h_kv, a.n_kv, a.hdr, a.k16,
-                     a.v16);
+    kv_pass<D, true, WIN>(b, a.kv_blocks, a.k, a.v, a.cu, a.n, a.ext, a.h_kv, a.n_kv, a.hdr,
+                          a.k16, a.v16, a.win);
   else
     pre_pass<D>(b - a.kv_blocks, a.q, a.o, a.dout, a.lse, a.tiles, a.h_q, a.n_q, a.n_kv, a.nq_pad,
                 a.scale, a.hdr, a.rec, a.stats);
@@ -727,92 +726,19 @@ __global__ __launch_bounds__(256) void bwd_copy_kernel(BwdPass a) {
 
 // ---------------------------------------------------------------------------
 // dK / dV kernel.
-template <int D>
-struct KvShape {
-  static constexpr int Q_EL = kRows * D;
-  static constexpr int HEAD_EL = rec_els(D);                  // Q, dO, aug of one head
-  static constexpr int STAGE_EL = 2 * HEAD_EL;                // a step is two query heads
-  static constexpr int NSTAGE = 4;                            // LDS ring of steps
-  static_assert((NSTAGE & (NSTAGE - 1)) == 0, "ring index by mask");
-  static constexpr int LOADS = STAGE_EL / 512 / kWaves;       // 1 KiB copies per wave per step
-  static_assert(LOADS * 512 * kWaves == STAGE_EL, "every wave copies as much");
-  static constexpr size_t SMEM = NSTAGE * STAGE_EL * sizeof(bf16);
-  static_assert((NSTAGE - 2) * LOADS <= 63, "vmcnt range");
-};
-
-// Walks the steps (32-row query block x two query heads) that attend one KV
-// block: tiles in list order, query blocks in row order, heads in order.  Per
-// fragment (one tile's rows of the sample) everything a step needs is
-// precomputed, so that advancing is a few 32-bit scalar operations plus one
-// running 64-bit record offset.
-struct StepIter {
-  const libra_tile_t *tiles;
-  int64_t T, n_q, n_kv, key0, p0, p1;   // rows at positions [p0, p1)
-  int h_q, g, G, kloc0, rkib;   // rkib: KiB of a record
-  // fragment
-  int64_t t;                // tile index
-  int nm, lo0, hin, qb0;    // blocks; lo of block 0; hi of the last block; q_loc of its row 0
-  int h0, h1;
-  // position
-  int mi, h;
-  int64_t rec;              // offset of the record of (block, h), in KiB
-  bool valid;
-
-  __device__ bool seek() {
-    for (; t < T; ++t) {
-      const libra_tile_t tl = tiles[t];
-      if (!tile_ok(tl, n_q, n_kv, h_q)) continue;
-      const int64_t pb = tl.q_begin > p0 ? tl.q_begin : p0;
-      const int64_t pe = tl.q_end < p1 ? tl.q_end : p1;
-      if (pb >= pe) continue;
-      h0 = max(tl.head_begin, g * G);
-      h1 = min(tl.head_end, (g + 1) * G);
-      if (h0 >= h1) continue;
-      const int64_t fra = tl.q_row + (pb - tl.q_begin);
-      const int64_t frb = fra + (pe - pb);
-      const int64_t qla = pb - key0;
-      const int64_t first = fra + (kloc0 > qla ? kloc0 - qla : 0);
-      if (first >= frb) continue;
-      const int64_t mf = first / kRows, ml = (frb - 1) / kRows;
-      const int64_t row0 = mf * kRows;
-      nm = (int)(ml - mf + 1);
-      lo0 = (int)(fra > row0 ? fra - row0 : 0);
-      hin = (int)(frb - ml * kRows);
-      qb0 = (int)(qla - (fra - row0));
-      mi = 0;
-      h = h0;
-      rec = (mf * h_q + h0) * rkib;
-      return true;
-    }
-    return false;
-  }
-  __device__ void start() { t = 0; valid = seek(); }
-  // steps are pairs of query heads (h, h + 1); two() is false for the last
-  // step of an odd head count
-  __device__ void next() {
-    if ((h += 2) < h1) {
-      rec += 2 * rkib;
-      return;
-    }
-    rec += (int64_t)((h_q - (h - 2 - h0)) * rkib);   // back by the heads advanced within this block
-    h = h0;
-    if (++mi < nm) return;
-    ++t;
-    valid = seek();
-  }
-  __device__ bool two() const { return h + 1 < h1; }
-  __device__ int lo() const { return mi == 0 ? lo0 : 0; }
-  __device__ int hi() const { return mi == nm - 1 ? hin : kRows; }
-  __device__ int qb() const { return qb0 + kRows * mi; }        // q_loc of the block's row 0
-};
-
-template <int D>
+// WIN: windowed attention.  An item's rows end with the window of its last key (for sink
+// keys of a sample that is not a far one, with the sample); the rows that a key's
+// window leaves out are masked like those before it.  The sums of a far sample's sinks
+// over the rows past their windows come from win_sink_kernel and are added at the end.
+template <int D, bool WIN>
 __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 1))) void attn_bwd_dkdv_kernel(
     const f16 *__restrict__ k, const f16 *__restrict__ v, const f16 *__restrict__ rec,
     const int64_t *__restrict__ cu, const libra_tile_t *__restrict__ tiles, int64_t T,
     const BwdItem *__restrict__ items, int32_t *__restrict__ hdr, int h_q, int h_kv,
     int64_t n_q, int64_t n_kv, float scale, float c2, void *__restrict__ dk_out,
-    void *__restrict__ dv_out, int accumulate, float *__restrict__ parts) {
+    void *__restrict__ dv_out, int accumulate, float *__restrict__ parts, Window win,
+    const WinSample *__restrict__ samples, const WinSink *__restrict__ sinks,
+    const float *__restrict__ sink_parts) {
   using S = KvShape<D>;
   extern __shared__ __attribute__((aligned(16))) bf16 smem[];
   __shared__ int32_t s_item;
@@ -854,7 +780,8 @@ __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 
 
   for (;;) {
     if (w == 0) {
-      const int got = take_item(hdr, kBwdQ, q_serve, q_state);
+      const int got = WIN ? take_run_item(hdr, kBwdQ, q_serve, q_state)
+                          : take_item(hdr, kBwdQ, q_serve, q_state);
       if (tid == 0) s_item = got;
     }
     __syncthreads();
@@ -862,7 +789,11 @@ __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 
     if (idx < 0) break;
     const BwdItem item = items[idx];
     const int64_t key0 = cu[item.sample];
-    const int64_t len = cu[item.sample + 1] - key0;
+    const int64_t full_len = cu[item.sample + 1] - key0;
+    // keys past the last covered row get no gradient
+    const int64_t len = WIN ? (int64_t)samples[item.sample].ext : full_len;
+    const bool far = WIN && far_sample(win, full_len);   // its sinks' far rows are not walked here
+    const int near_sinks = far ? 0 : win.sinks;
     const int g = item.g;
     const int kloc0 = item.kb * kBwdBK;
     const int kw0 = kloc0 + 32 * w;                   // first key of this wave
@@ -1116,9 +1047,9 @@ __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 
     // Steps are walked once, at issue; what the compute side needs of the step
     // in ring stage j (lo | hi << 8 | two << 16, and the q_loc of the block's
     // row 0) waits in lane j of desc / desc_qb.
-    StepIter iss{tiles, T, n_q, n_kv, key0, key0 + item.r0,
+    StepIter iss{tiles, WIN ? (int64_t)item.t1 + 1 : T, n_q, n_kv, key0, key0 + item.r0,
                  key0 + (item.r1 < len ? item.r1 : len), h_q, g, G, kloc0, 2 * S::HEAD_EL / 1024};
-    iss.start();
+    iss.start(WIN ? item.t0 : 0);
     int desc = 0, desc_qb = 0;
     int issued = 0, computed = 0;
     // ring stage and descriptor of the next step to copy; after the last one,
@@ -1159,13 +1090,20 @@ __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 
         const int lo_l = dsc & 0xff, hi_l = (dsc >> 8) & 0xff;
         const bool two = (dsc >> 16) != 0;
         const int qb = __builtin_amdgcn_readlane(desc_qb, sg);   // q_loc of the block's row 0
-        if (kw0 <= qb + hi_l - 1) {
+        bool mine = kw0 <= qb + hi_l - 1;
+        // the window of the block's first row starts past the wave's keys
+        if constexpr (WIN) mine = mine && (qb + lo_l - (kw0 + 31) < win.size || kw0 < near_sinks);
+        if (mine) {
           const bf16 *Qs = smem + sg * S::STAGE_EL;
           // interior blocks: every row inside the fragment and at or after every key
-          const bool full = lo_l == 0 && hi_l == kRows && wave_keys_ok && kw0 + 31 <= qb;
+          bool full = lo_l == 0 && hi_l == kRows && wave_keys_ok && kw0 + 31 <= qb;
+          if constexpr (WIN) full = full && (qb + 31 - kw0 < win.size || kw0 + 31 < near_sinks);
           const int need = kl - qb;                               // first iq with q_loc >= kl
           const int lower = need > lo_l ? (need < kRows ? need : kRows) : lo_l;
-          const int upper = key_ok ? hi_l : 0;
+          int upper = key_ok ? hi_l : 0;
+          // rows up to kl + size - 1; kl - qb <= 31, and size <= n_kv
+          if constexpr (WIN)
+            if (kl >= near_sinks) upper = min(upper, kl - qb + win.size);
           if constexpr (decltype(pairs_t)::value) {
             step2(full, Qs, lower, upper);
           } else {
@@ -1185,6 +1123,25 @@ __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 
       // against 92.5 to 92.6
       align_code<5>();
       steps(std::true_type{});
+    }
+
+    if constexpr (WIN) {
+      // the far rows of this wave's sinks (places as written by win_sink_sum_kernel)
+      const int first = samples[item.sample].far;   // -1: no far row is covered
+      if (first >= 0 && kw0 < win.sinks) {
+        const WinSink sk = sinks[first + g * sink_blocks(win) + kw0 / 32];
+        if (sk.parts > 0) {
+          const float *src = sink_parts + (size_t)sk.base * sink_part_floats(D) +
+                             (size_t)ln * D + 8 * kg;
+          static_for<D / 32>([&](auto dt) {
+            static_for<16>([&](auto r) {
+              constexpr int at = 32 * dt + 16 * (r >> 3) + (r & 7);
+              dka[dt][int(r)] += src[at];
+              dva[dt][int(r)] += src[32 * D + at];
+            });
+          });
+        }
+      }
     }
 
     // ---- write dK, dV for this wave's 32 keys
@@ -1302,17 +1259,21 @@ __global__ __launch_bounds__(256) void bwd_dkdv_combine_kernel(
 // ---------------------------------------------------------------------------
 static size_t align256b(size_t x) { return (x + 255) / 256 * 256; }
 
-BwdLayout bwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d) {
+BwdLayout bwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d,
+                     const Window &win) {
   BwdLayout L;
+  const bool w = win.size > 0;
+  const int64_t key_blocks = n_kv / kBwdBK + n + 1;
   // a split item's parts take its place: kBwdSplitSlots of them at most
-  L.max_blocks = (n_kv / kBwdBK + n + 1) * (int64_t)h_kv;
-  L.max_items = L.max_blocks + kBwdSplitSlots;
+  L.max_blocks = key_blocks * (int64_t)h_kv;
+  L.max_items = L.max_blocks + (w ? 0 : kBwdSplitSlots);
   L.max_qitems = fwd_max_items(T, n, n_q, h_q, h_kv);
   L.nq_pad = (n_q + kRows - 1) / kRows * kRows;
   L.hdr = 0;
   L.ext = kHdrBytes;
-  L.gmask = align256b(L.ext + (size_t)n * sizeof(int32_t));
-  L.items = align256b(L.gmask + (size_t)n * sizeof(unsigned long long));
+  L.gmask = align256b(L.ext + (size_t)n * (w ? sizeof(WinSample) : sizeof(int32_t)));
+  L.items = align256b(L.gmask + (w ? (size_t)key_blocks * sizeof(WinBlock)
+                                   : (size_t)n * sizeof(unsigned long long)));
   L.qitems = align256b(L.items + (size_t)L.max_items * sizeof(BwdItem));
   L.rec = align256b(L.qitems + (size_t)L.max_qitems * sizeof(FwdItem));
   // one record more: a step of one head copies the record after its own
@@ -1322,22 +1283,35 @@ BwdLayout bwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, i
   L.splits = align256b(L.stats + (size_t)h_q * L.nq_pad * 2 * sizeof(float));
   L.max_parts = kFwdSplitSlots;
   L.bsplits = align256b(L.splits + (size_t)(L.max_parts / 2) * sizeof(FwdSplit));
-  L.cov = align256b(L.bsplits + (size_t)(kBwdSplitSlots / 2) * sizeof(BwdSplit));
-  // the partial slots serve the dQ kernel, then the dK / dV kernel
-  L.parts = align256b(L.cov + (size_t)L.max_blocks * 2 * sizeof(int32_t));
+  if (w) {
+    // far samples lie side by side, so there are few of them
+    const int64_t far = win.sinks ? std::min(n, n_kv / ((int64_t)win.size + kFarRows + 1)) : 0;
+    const int64_t sinks = far * h_kv * sink_blocks(win);
+    const int64_t slots = far ? sinks + kSinkParts : 0;
+    L.far_list = align256b(L.bsplits + (size_t)sinks * sizeof(WinSink));
+    L.sink_items = align256b(L.far_list + (size_t)far * sizeof(int32_t));
+    L.sink_parts = align256b(L.sink_items + (size_t)slots * sizeof(BwdItem));
+    L.parts = align256b(L.sink_parts + (size_t)slots * sink_part_floats(d) * sizeof(float));
+    L.far = far;
+  } else {
+    L.cov = align256b(L.bsplits + (size_t)(kBwdSplitSlots / 2) * sizeof(BwdSplit));
+    // the partial slots serve the dQ kernel, then the dK / dV kernel
+    L.parts = align256b(L.cov + (size_t)L.max_blocks * 2 * sizeof(int32_t));
+  }
   L.total = align256b(L.parts + (size_t)L.max_parts * fwd_part_floats(d) * sizeof(float));
   return L;
 }
 
-template <int D>
+template <int D, bool WIN>
 static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o,
                         const float *lse, const bf16 *dout, const int64_t *cu, int64_t n,
                         const libra_tile_t *tiles, int64_t T, int64_t n_q, int64_t n_kv, int h_q,
                         int h_kv, float scale, bf16 *dq, void *dk, void *dv, bool accumulate,
                         char *ws, const BwdLayout &L, hipStream_t st, const KernelTimer *tm_kv,
-                        const KernelTimer *tm_q) {
+                        const KernelTimer *tm_q, bool exact_o, const Window &win) {
   int32_t *hdr = reinterpret_cast<int32_t *>(ws + L.hdr);
   int32_t *ext = reinterpret_cast<int32_t *>(ws + L.ext);
+  auto *samples = reinterpret_cast<WinSample *>(ws + L.ext);   // WIN
   auto *gmask = reinterpret_cast<unsigned long long *>(ws + L.gmask);
   BwdItem *items = reinterpret_cast<BwdItem *>(ws + L.items);
   FwdItem *qitems = reinterpret_cast<FwdItem *>(ws + L.qitems);
@@ -1348,7 +1322,7 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
   int32_t *cov = reinterpret_cast<int32_t *>(ws + L.cov);
   static bool attr_set = false;
   if (!attr_set) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_bwd_dkdv_kernel<D>),
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_bwd_dkdv_kernel<D, WIN>),
                             hipFuncAttributeMaxDynamicSharedMemorySize,
                             (int)KvShape<D>::SMEM) != hipSuccess)
       return fail(LIBRA_EHIP, "hipFuncSetAttribute failed");
@@ -1374,13 +1348,26 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
     // 3-5% from it
     auto *splits = reinterpret_cast<FwdSplit *>(ws + L.splits);
     float *parts = reinterpret_cast<float *>(ws + L.parts);
-    const int max_parts = may_split(n_kv) ? L.max_parts : 0;
-    hipLaunchKernelGGL(prep_bwd_kernel, dim3(2), dim3(kPrepThreads), 0, st,
-                       BwdPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, hdr, ext, gmask, items,
-                               L.max_items, cus, reinterpret_cast<BwdSplit *>(ws + L.bsplits), cov,
-                               cov + L.max_blocks},
-                       FwdPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, hdr, qitems, L.max_qitems, 0,
-                               cus, cus, max_parts, 1, splits});
+    int max_parts;
+    WinBwdPrep wb{};
+    if constexpr (WIN) {
+      max_parts = win_may_split(win, n_kv) ? L.max_parts : 0;
+      wb = WinBwdPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, win, hdr, samples,
+                      reinterpret_cast<WinBlock *>(ws + L.gmask), L.max_blocks / h_kv, items,
+                      L.max_items, reinterpret_cast<WinSink *>(ws + L.bsplits),
+                      reinterpret_cast<int32_t *>(ws + L.far_list),
+                      reinterpret_cast<BwdItem *>(ws + L.sink_items)};
+      launch_win_prep_bwd(WinPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, win, hdr, qitems,
+                                  L.max_qitems, 0, cus, cus, max_parts, 1, splits}, wb, cus, st);
+    } else {
+      max_parts = may_split(n_kv) ? L.max_parts : 0;
+      hipLaunchKernelGGL(prep_bwd_kernel, dim3(2), dim3(kPrepThreads), 0, st,
+                         BwdPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, hdr, ext, gmask, items,
+                                 L.max_items, cus, reinterpret_cast<BwdSplit *>(ws + L.bsplits),
+                                 cov, cov + L.max_blocks},
+                         FwdPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, hdr, qitems, L.max_qitems,
+                                 0, cus, cus, max_parts, 1, splits});
+    }
     // K and V rows: at least eight for a wave (every workgroup that finds a new
     // maximum posts an atomic on the same two slots: 2048 of them took 24 us on
     // 4096 rows)
@@ -1389,22 +1376,28 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
     const BwdPass pass{q, k, v, o, dout, lse, cu, n, tiles, h_q, h_kv, n_q, n_kv, L.nq_pad, scale,
                        hdr, ext, rec, k16, v16, stats, static_cast<uint4 *>(dk),
                        static_cast<uint4 *>(dv), n16, (unsigned)(T * kTileSplit), kv_blocks,
-                       2 * zero_blocks};
-    hipLaunchKernelGGL(bwd_max_kernel<D>,
+                       2 * zero_blocks, win};
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(bwd_max_kernel<D, WIN>),
                        dim3(pass.kv_blocks + pass.tile_blocks + pass.zero_blocks), dim3(256), 0,
                        st, pass);
-    hipLaunchKernelGGL(bwd_copy_kernel<D>, dim3(pass.kv_blocks + pass.tile_blocks), dim3(256), 0,
-                       st, pass);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(bwd_copy_kernel<D, WIN>),
+                       dim3(pass.kv_blocks + pass.tile_blocks), dim3(256), 0, st, pass);
     // dQ first: it writes the -D records the dK / dV kernel reads
     const int rc = launch_bwd_dq(D, q, dout, k, v, stats, cu, qitems, hdr, h_q, h_kv, n_q, n_kv,
                                  L.nq_pad, scale, dq, rec, splits, parts, max_parts, cus,
-                                 st, tm_q);
+                                 st, tm_q, exact_o ? 1.f : 0.f, win);
     if (rc != LIBRA_OK) return rc;
     if (tm_kv) hipEventRecord(tm_kv->begin, st);
-    hipLaunchKernelGGL(attn_bwd_dkdv_kernel<D>, dim3(cus), dim3(kThreads), KvShape<D>::SMEM, st,
-                       k16, v16, rec, cu, tiles, T, items, hdr, h_q, h_kv, n_q, n_kv, scale,
-                       scale * kLog2e, dk, dv, accumulate ? 1 : 0, parts);
-    if (may_split_rows(n_kv))
+    float *sink_parts = reinterpret_cast<float *>(ws + L.sink_parts);
+    if constexpr (WIN)
+      if (L.far > 0)
+        if (int e = launch_win_sinks(D, k16, v16, rec, wb, scale * kLog2e, sink_parts, cus, st))
+          return e;
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(attn_bwd_dkdv_kernel<D, WIN>), dim3(cus), dim3(kThreads),
+                       KvShape<D>::SMEM, st, k16, v16, rec, cu, tiles, T, items, hdr, h_q, h_kv,
+                       n_q, n_kv, scale, scale * kLog2e, dk, dv, accumulate ? 1 : 0, parts, win,
+                       samples, wb.sinks, sink_parts);
+    if (!WIN && may_split_rows(n_kv))
       hipLaunchKernelGGL(bwd_dkdv_combine_kernel<D>, dim3(cus * 4), dim3(256), 0, st,
                          reinterpret_cast<const BwdSplit *>(ws + L.bsplits), hdr, parts, cu, h_kv,
                          scale, dk, dv, accumulate ? 1 : 0);
@@ -1419,19 +1412,15 @@ int launch_bwd(const void *q, const void *k, const void *v, const void *o, const
                const void *dout, const int64_t *cu, int64_t n, const libra_tile_t *tiles,
                int64_t T, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d, float scale,
                void *dq, void *dk, void *dv, bool accumulate, void *ws, const BwdLayout &L,
-               hipStream_t st, const KernelTimer *tm_kv, const KernelTimer *tm_q) {
-  auto Q = static_cast<const bf16 *>(q);
-  auto K = static_cast<const bf16 *>(k);
-  auto V = static_cast<const bf16 *>(v);
-  auto O = static_cast<const bf16 *>(o);
-  auto dO = static_cast<const bf16 *>(dout);
-  auto dQ = static_cast<bf16 *>(dq);
-  char *W = static_cast<char *>(ws);
-  if (d == 128)
-    return launch_bwd_d<128>(Q, K, V, O, lse, dO, cu, n, tiles, T, n_q, n_kv, h_q, h_kv, scale,
-                             dQ, dk, dv, accumulate, W, L, st, tm_kv, tm_q);
-  return launch_bwd_d<64>(Q, K, V, O, lse, dO, cu, n, tiles, T, n_q, n_kv, h_q, h_kv, scale, dQ,
-                          dk, dv, accumulate, W, L, st, tm_kv, tm_q);
+               hipStream_t st, const KernelTimer *tm_kv, const KernelTimer *tm_q, bool exact_o,
+               const Window &win) {
+  const auto launch = d == 128 ? (win.size ? launch_bwd_d<128, true> : launch_bwd_d<128, false>)
+                               : (win.size ? launch_bwd_d<64, true> : launch_bwd_d<64, false>);
+  return launch(static_cast<const bf16 *>(q), static_cast<const bf16 *>(k),
+                static_cast<const bf16 *>(v), static_cast<const bf16 *>(o), lse,
+                static_cast<const bf16 *>(dout), cu, n, tiles, T, n_q, n_kv, h_q, h_kv, scale,
+                static_cast<bf16 *>(dq), dk, dv, accumulate, static_cast<char *>(ws), L, st, tm_kv,
+                tm_q, exact_o, win);
 }
 
 }  // namespace libra

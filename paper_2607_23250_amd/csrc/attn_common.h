@@ -51,6 +51,7 @@ enum HdrSlot {
   kBwdQ = 32,      // dK/dV work items
   kMaxAbs = 56,    // backward: max |x| (fp32 bits) of Q, dO, K, V in slots 56..59
   kFwdSplits = 60, // forward: split items (FwdSplit records), then partial slots used (61)
+  kSinkItems = 62, // windowed backward: items of the sinks' far rows, then WinSink records (63)
   kFwdHeads = 64,  // queue heads of the forward / dQ work items
   kHdrSlots = kFwdHeads + kXcds * 32
 };
@@ -200,6 +201,68 @@ __device__ __forceinline__ int take_item(int32_t *hdr, int base, int q, int &sta
   }
 }
 
+// Items of about equal cost (windowed attention) stay in one list of hdr[base +
+// kXcds] entries (at most hdr[base + 2 kXcds]) instead of a sorted segment per queue: runs of 2^shift
+// neighbours, which read the same K / V rows or query blocks, go to the XCDs in
+// turn.  Queue x holds the items of its runs, in list order.
+__host__ __device__ constexpr int run_shift(int n) { return n >= 4096 ? 6 : n >= 512 ? 3 : 0; }
+__device__ __forceinline__ int run_count(int n, int sh, int x) {
+  const int rest = (n & ((kXcds << sh) - 1)) - (x << sh);
+  return (n >> (sh + 3) << sh) + max(0, min(rest, 1 << sh));
+}
+__device__ __forceinline__ int run_index(int sh, int x, int r) {
+  return ((r >> sh) * kXcds + x << sh) + (r & ((1 << sh) - 1));
+}
+static_assert(kXcds == 8, "run_count divides by 8");
+
+// take_item for such a list: the same protocol and the same heads.
+__device__ __forceinline__ int take_run_item(int32_t *hdr, int base, int q, int &state) {
+  int32_t *set = hdr + base;
+  asm volatile("" : "+s"(set));
+  const int lane = threadIdx.x & 63;
+  const int n = min(set[kXcds], set[2 * kXcds]), sh = run_shift(n);
+  if (state == kTakeFirst) {
+    const int x = blockIdx.x % kXcds, r = blockIdx.x / kXcds;
+    const bool got = r < run_count(n, sh, x);
+    state = got ? kTakeOwn : kTakeOther;
+    if (got) return run_index(sh, x, r);
+  }
+  for (int x = q;;) {
+    if (state == kTakeOther) {
+      const int lx = lane & (kXcds - 1);
+      const bool some = lane < kXcds && ld_agent(&set[head_slot(base, lx) - base]) <
+                                            run_count(n, sh, lx);
+      const uint32_t m = (uint32_t)__builtin_amdgcn_ballot_w64(some);
+      if (m == 0) return -1;
+      x = (q + __builtin_ctz((m | m << kXcds) >> q)) & (kXcds - 1);
+    }
+    int got = 0;
+    if (lane == 0) got = atomicAdd(&set[head_slot(base, x) - base], 1);
+    got = __builtin_amdgcn_readfirstlane(got);
+    if (got < run_count(n, sh, x)) return run_index(sh, x, got);
+    state = kTakeOther;
+  }
+}
+
+// Windowed attention: the row at sample-local position p attends the keys
+// p - size + 1 .. p and the keys below `sinks` (both at most n_kv).
+struct Window {
+  int32_t size = 0;    // 0: no window (plain causal attention)
+  int32_t sinks = 0;
+};
+// A sample whose rows reach this far past the window of its first key has the
+// gradients of its sink keys summed over those far rows by a kernel of their
+// own; in shorter ones the far rows are part of the sink keys' dK / dV items.
+constexpr int kFarRows = 512;
+__host__ __device__ __forceinline__ bool far_sample(const Window &w, int64_t len) {
+  return w.sinks > 0 && len > (int64_t)w.size + kFarRows;
+}
+// The item walks its key blocks as steps: `far` blocks of sinks from key 0 on,
+// then, `gap` blocks later, those of the window.
+__device__ __forceinline__ int step_block(int step, int far, int gap) {
+  return step < far ? step : step + gap;
+}
+
 // One forward work item: up to 4 query heads of one KV group x up to
 // 32 * (4 / heads) consecutive rows of one sample fragment of one tile.
 // An item walks the 64-key blocks [kb0, kb1) of its rows' sample; a whole
@@ -218,7 +281,7 @@ struct FwdItem {
   int32_t kb0;      // first key block
   int32_t kb1;      // end of the key blocks
   int32_t slot;     // partial slot of a split part, or -1
-  int32_t pad0, pad1;
+  int32_t far, gap;   // windowed: kb0 and kb1 count steps (step_block)
 };
 static_assert(sizeof(FwdItem) == 48, "item layout");
 
@@ -262,7 +325,7 @@ struct BwdItem {
   int32_t slot;
   int32_t r0;
   int32_t r1;
-  int32_t pad0, pad1;
+  int32_t t0, t1;   // windowed: the tiles with rows of the item are among [t0, t1]
 };
 static_assert(sizeof(BwdItem) == 32, "item layout");
 // A split dK / dV item and its partial slots [base, base + parts), in row order.
@@ -657,6 +720,9 @@ struct FwdLayout {
 struct BwdLayout {
   size_t hdr = 0, ext = 0, gmask = 0, items = 0, qitems = 0, rec = 0, k16 = 0,
          v16 = 0, stats = 0, splits = 0, bsplits = 0, cov = 0, parts = 0, total = 0;
+  // windowed: WinSample records at ext, WinBlock at gmask, WinSink at bsplits
+  size_t far_list = 0, sink_items = 0, sink_parts = 0;
+  int64_t far = 0;   // far samples at most
   int32_t max_parts = 0;   // split-K partial slots of the dQ kernel
   int64_t max_blocks = 0, max_items = 0, max_qitems = 0, nq_pad = 0;
 };
@@ -665,7 +731,8 @@ struct BwdLayout {
 // forward never splits an item (the allocation-free entry point).
 FwdLayout fwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d,
                      bool split = true);
-BwdLayout bwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d);
+BwdLayout bwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d,
+                     const Window &win = {});
 
 // Optional HIP events recorded around a main kernel (see libra_timing_*).
 struct KernelTimer {
@@ -677,18 +744,21 @@ int64_t fwd_max_items(int64_t T, int64_t n, int64_t n_q, int h_q, int h_kv);
 int launch_fwd(const void *q, const void *k, const void *v, const int64_t *cu, int64_t n,
                const libra_tile_t *tiles, int64_t T, int64_t n_q, int64_t n_kv, int h_q,
                int h_kv, int d, float scale, void *o, float *lse, void *ws,
-               const FwdLayout &L, hipStream_t st, const KernelTimer *tm);
+               const FwdLayout &L, hipStream_t st, const KernelTimer *tm,
+               const Window &win = {});
 // The dQ kernel of the backward pass (attn_bwd_dq.hip), on `blocks`
 // persistent workgroups over the forward-style work items.
 int launch_bwd_dq(int d, const bf16 *q, const bf16 *dout, const bf16 *k, const bf16 *v,
                   const float *stats, const int64_t *cu, const FwdItem *items, int32_t *hdr,
                   int h_q, int h_kv, int64_t n_q, int64_t n_kv, int64_t nq_pad, float scale,
                   bf16 *dq, f16 *rec, const FwdSplit *splits, float *parts, int max_parts,
-                  int blocks, hipStream_t st, const KernelTimer *tm);
+                  int blocks, hipStream_t st, const KernelTimer *tm, float d_fix,
+                  const Window &win);
 int launch_bwd(const void *q, const void *k, const void *v, const void *o, const float *lse,
                const void *dout, const int64_t *cu, int64_t n, const libra_tile_t *tiles,
                int64_t T, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d, float scale,
                void *dq, void *dk, void *dv, bool accumulate, void *ws, const BwdLayout &L,
-               hipStream_t st, const KernelTimer *tm_kv, const KernelTimer *tm_q);
+               hipStream_t st, const KernelTimer *tm_kv, const KernelTimer *tm_q,
+               bool exact_o = true, const Window &win = {});   // exact_o: see d_fix of dQ
 
 }  // namespace libra
