@@ -190,7 +190,7 @@ int attn_bwd(const void *q, const void *k, const void *v, const void *o, const f
              const libra_tile_t *tiles, int64_t num_tiles, int64_t n_q_rows, int64_t n_kv_rows,
              int32_t h_q, int32_t h_kv, int32_t head_dim, float softmax_scale, void *dq, void *dk,
              void *dv, uint32_t flags, void *workspace, const BwdLayout &L, void *stream,
-             bool exact_o, const Window &win) {
+             bool exact_o, const Window &win, const Held &q8 = {}, const Held &o8 = {}) {
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.f / std::sqrt((float)head_dim);
   int rc = LIBRA_OK;
   const KernelTimer *tm_kv = num_tiles > 0 ? next_timer(1, &rc) : nullptr;
@@ -200,7 +200,7 @@ int attn_bwd(const void *q, const void *k, const void *v, const void *o, const f
   return launch_bwd(q, k, v, o, lse, dout, cu_seqlens, num_samples, tiles, num_tiles, n_q_rows,
                     n_kv_rows, h_q, h_kv, head_dim, scale, dq, dk, dv,
                     (flags & LIBRA_BWD_ACCUMULATE_DKV) != 0, workspace, L,
-                    static_cast<hipStream_t>(stream), tm_kv, tm_q, exact_o, win);
+                    static_cast<hipStream_t>(stream), tm_kv, tm_q, exact_o, win, q8, o8);
 }
 
 }  // namespace
@@ -356,7 +356,8 @@ int check_ckpt8(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_
   return LIBRA_OK;
 }
 
-// Workspace of libra_attn_bwd_ckpt8: the unpacked q, k, v, o, then a backward's.
+// Workspace of libra_attn_bwd_ckpt8: the unpacked k and v, for a causal call q and o too
+// (the windowed kernels read them as they are), then a backward's.
 struct Ckpt8Layout {
   size_t at[4], bwd = 0, total = 0;
   BwdLayout L;
@@ -366,7 +367,8 @@ Ckpt8Layout ckpt8_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_
                          const Window &win) {
   Ckpt8Layout c;
   c.L = bwd_layout(T, n, n_q, n_kv, h_q, h_kv, d, win);
-  const size_t q = align256((size_t)n_q * h_q * d * 2), k = align256((size_t)n_kv * h_kv * d * 2);
+  const size_t q = win.size ? 0 : align256((size_t)n_q * h_q * d * 2);
+  const size_t k = align256((size_t)n_kv * h_kv * d * 2);
   c.at[0] = 0;
   c.at[1] = q;
   c.at[2] = q + k;
@@ -431,20 +433,23 @@ extern "C" int libra_attn_bwd_ckpt8(const libra_ckpt8_t *q, const libra_ckpt8_t 
     const libra_ckpt8_t *in[4] = {q, k, v, o};
     Ckpt8Four four;
     for (int i = 0; i < 4; ++i) {
-      const int64_t chunks = (i == 0 || i == 3 ? n_q_rows * h_q : n_kv_rows * h_kv) * head_dim / 16;
+      const bool rows = i == 0 || i == 3;
+      const int64_t chunks = (rows ? n_q_rows * h_q : n_kv_rows * h_kv) * head_dim / 16;
       if (chunks && (!in[i]->q || !in[i]->e)) return fail(LIBRA_EINVAL, "NULL checkpoint pointer");
       if (reinterpret_cast<uintptr_t>(in[i]->q) % 16)
         return fail(LIBRA_EINVAL, "checkpoint integers must be 16-byte aligned");
       four.q[i] = in[i]->q;
       four.e[i] = in[i]->e;
       four.x[i] = reinterpret_cast<bf16 *>(ws + C.at[i]);
-      four.chunks[i] = chunks;
+      four.chunks[i] = rows && win.size ? 0 : chunks;
     }
     if (int rc = check_ws(workspace, workspace_bytes, C.total)) return rc;
     if (int rc = launch_ckpt8_unpack4(four, static_cast<hipStream_t>(stream))) return rc;
   }
-  return attn_bwd(ws + C.at[0], ws + C.at[1], ws + C.at[2], ws + C.at[3], lse, dout, cu_seqlens,
-                  num_samples, tiles, num_tiles, n_q_rows, n_kv_rows, h_q, h_kv, head_dim,
-                  softmax_scale, dq, dk, dv, flags, num_tiles > 0 ? ws + C.bwd : ws, C.L, stream,
-                  false, win);
+  const bool as_held = win.size > 0 && num_tiles > 0;
+  return attn_bwd(as_held ? nullptr : ws + C.at[0], ws + C.at[1], ws + C.at[2],
+                  as_held ? nullptr : ws + C.at[3], lse, dout, cu_seqlens, num_samples, tiles,
+                  num_tiles, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, softmax_scale, dq, dk, dv,
+                  flags, num_tiles > 0 ? ws + C.bwd : ws, C.L, stream, false, win,
+                  as_held ? Held{q->q, q->e} : Held{}, as_held ? Held{o->q, o->e} : Held{});
 }

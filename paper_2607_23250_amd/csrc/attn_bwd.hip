@@ -486,8 +486,11 @@ constexpr int kTileSplit = 64;
 // kernel stages whole records; rows no tile covers must hold finite values,
 // since they meet P = dS = 0 in its products).  So must the -D operand of a tile's
 // rows past the last sample (position `pool` on), which no dQ item writes.
-template <int D>
+// WIN: nor does any write the other parts of those rows (the dQ kernel writes the records
+// there).  HELD: q in 8 bits.
+template <int D, bool WIN, bool HELD>
 __device__ __forceinline__ void absmax_q(unsigned block, const bf16 *__restrict__ q,
+                                         const Held &q8,
                                          const bf16 *__restrict__ dout,
                                          const libra_tile_t *__restrict__ tiles, int h_q,
                                          int64_t n_q, int64_t n_kv, int64_t pool,
@@ -501,7 +504,23 @@ __device__ __forceinline__ void absmax_q(unsigned block, const bf16 *__restrict_
   float mq = 0.f, mo = 0.f;
   for (int64_t m = ra / kRows + block % kTileSplit; m * kRows < rb; m += kTileSplit) {
     const int64_t row = m * kRows + r;
-    const bool ok = row >= ra && row < rb;
+    const bool ok = row >= ra && row < rb && !(WIN && row >= past);
+    if constexpr (WIN) {
+      // several heads' loads at once: the pass is bound by them (537 MB of Q and dO with
+      // 153 us one head at a time)
+      if (ok) {
+#pragma unroll 4
+        for (int h = tl.head_begin; h < tl.head_end; ++h) {
+          const size_t off = ((size_t)row * h_q + h) * D + part * (D / 8);
+          static_for<D / 64>([&](auto c) {
+            if constexpr (HELD) mq = fmaxf(mq, absmax8(held8(q8, off + 8 * c)));
+            else mq = fmaxf(mq, absmax8(*reinterpret_cast<const bf16x8 *>(q + off + 8 * c)));
+            mo = fmaxf(mo, absmax8(*reinterpret_cast<const bf16x8 *>(dout + off + 8 * c)));
+          });
+        }
+        continue;
+      }
+    }
     for (int h = tl.head_begin; h < tl.head_end; ++h) {
       f16 *rp = rec + ((size_t)m * h_q + h) * rec_els(D);
       f16x8 z;
@@ -697,8 +716,9 @@ struct BwdPass {
   int64_t n16;                             // 16-byte pieces of each
   unsigned tile_blocks, kv_blocks, zero_blocks;
   Window win;
+  Held q8;
 };
-template <int D, bool WIN>
+template <int D, bool WIN, bool HELD>
 __global__ __launch_bounds__(256) void bwd_max_kernel(BwdPass a) {
   unsigned b = blockIdx.x;
   if (b == 0 && threadIdx.x == 0 && a.hdr[kDqFull]) atomicAdd(&a.hdr[kBadTiles], 1);
@@ -706,7 +726,7 @@ __global__ __launch_bounds__(256) void bwd_max_kernel(BwdPass a) {
     kv_pass<D, false, WIN>(b, a.kv_blocks, a.k, a.v, a.cu, a.n, a.ext, a.h_kv, a.n_kv, a.hdr,
                            a.k16, a.v16, a.win);
   } else if ((b -= a.kv_blocks) < a.tile_blocks) {
-    absmax_q<D>(b, a.q, a.dout, a.tiles, a.h_q, a.n_q, a.n_kv, a.cu[a.n], a.hdr, a.rec);
+    absmax_q<D, WIN, HELD>(b, a.q, a.q8, a.dout, a.tiles, a.h_q, a.n_q, a.n_kv, a.cu[a.n], a.hdr, a.rec);
   } else {
     b -= a.tile_blocks;
     const unsigned half = a.zero_blocks / 2;
@@ -719,7 +739,7 @@ __global__ __launch_bounds__(256) void bwd_copy_kernel(BwdPass a) {
   if (b < a.kv_blocks)
     kv_pass<D, true, WIN>(b, a.kv_blocks, a.k, a.v, a.cu, a.n, a.ext, a.h_kv, a.n_kv, a.hdr,
                           a.k16, a.v16, a.win);
-  else
+  else if constexpr (!WIN)
     pre_pass<D>(b - a.kv_blocks, a.q, a.o, a.dout, a.lse, a.tiles, a.h_q, a.n_q, a.n_kv, a.nq_pad,
                 a.scale, a.hdr, a.rec, a.stats);
 }
@@ -1302,13 +1322,14 @@ BwdLayout bwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, i
   return L;
 }
 
-template <int D, bool WIN>
+template <int D, bool WIN, bool HELD>
 static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o,
                         const float *lse, const bf16 *dout, const int64_t *cu, int64_t n,
                         const libra_tile_t *tiles, int64_t T, int64_t n_q, int64_t n_kv, int h_q,
                         int h_kv, float scale, bf16 *dq, void *dk, void *dv, bool accumulate,
                         char *ws, const BwdLayout &L, hipStream_t st, const KernelTimer *tm_kv,
-                        const KernelTimer *tm_q, bool exact_o, const Window &win) {
+                        const KernelTimer *tm_q, bool exact_o, const Window &win, const Held &q8,
+                        const Held &o8) {
   int32_t *hdr = reinterpret_cast<int32_t *>(ws + L.hdr);
   int32_t *ext = reinterpret_cast<int32_t *>(ws + L.ext);
   auto *samples = reinterpret_cast<WinSample *>(ws + L.ext);   // WIN
@@ -1358,7 +1379,8 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
                       reinterpret_cast<int32_t *>(ws + L.far_list),
                       reinterpret_cast<BwdItem *>(ws + L.sink_items)};
       launch_win_prep_bwd(WinPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, win, hdr, qitems,
-                                  L.max_qitems, 0, cus, cus, max_parts, 1, splits}, wb, cus, st);
+                                  L.max_qitems, 0, cus * kWinDqPerCu, cus * kWinDqPerCu,
+                                  max_parts, 0, splits}, wb, cus, st);
     } else {
       max_parts = may_split(n_kv) ? L.max_parts : 0;
       hipLaunchKernelGGL(prep_bwd_kernel, dim3(2), dim3(kPrepThreads), 0, st,
@@ -1376,16 +1398,29 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
     const BwdPass pass{q, k, v, o, dout, lse, cu, n, tiles, h_q, h_kv, n_q, n_kv, L.nq_pad, scale,
                        hdr, ext, rec, k16, v16, stats, static_cast<uint4 *>(dk),
                        static_cast<uint4 *>(dv), n16, (unsigned)(T * kTileSplit), kv_blocks,
-                       2 * zero_blocks, win};
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(bwd_max_kernel<D, WIN>),
+                       2 * zero_blocks, win, q8};
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(bwd_max_kernel<D, WIN, HELD>),
                        dim3(pass.kv_blocks + pass.tile_blocks + pass.zero_blocks), dim3(256), 0,
                        st, pass);
     hipLaunchKernelGGL(HIP_KERNEL_NAME(bwd_copy_kernel<D, WIN>),
-                       dim3(pass.kv_blocks + pass.tile_blocks), dim3(256), 0, st, pass);
-    // dQ first: it writes the -D records the dK / dV kernel reads
-    const int rc = launch_bwd_dq(D, q, dout, k, v, stats, cu, qitems, hdr, h_q, h_kv, n_q, n_kv,
-                                 L.nq_pad, scale, dq, rec, splits, parts, max_parts, cus,
-                                 st, tm_q, exact_o ? 1.f : 0.f, win);
+                       dim3(pass.kv_blocks + (WIN ? 0 : pass.tile_blocks)), dim3(256), 0, st,
+                       pass);
+    // dQ first: it writes the -D records (windowed: all records) the dK / dV kernel reads
+    const float d_fix = exact_o ? 1.f : 0.f;
+    int rc;
+    if constexpr (WIN) {
+      if (tm_q) hipEventRecord(tm_q->begin, st);
+      rc = launch_win_dq(D, WinDq{q, o, dout, k, v, q8, o8, lse, qitems, hdr, h_q, h_kv, n_q,
+                                  L.nq_pad, scale, scale * kLog2e, d_fix, win, dq, rec, stats,
+                                  parts}, cus, st);
+      if (max_parts > 0)
+        launch_dq_combine(D, splits, hdr, parts, stats, h_q, L.nq_pad, scale, dq, rec, d_fix,
+                          cus * 4, st);
+      if (tm_q) hipEventRecord(tm_q->end, st);
+    } else {
+      rc = launch_bwd_dq(D, q, dout, k, v, stats, cu, qitems, hdr, h_q, h_kv, n_q, n_kv, L.nq_pad,
+                         scale, dq, rec, splits, parts, max_parts, cus, st, tm_q, d_fix);
+    }
     if (rc != LIBRA_OK) return rc;
     if (tm_kv) hipEventRecord(tm_kv->begin, st);
     float *sink_parts = reinterpret_cast<float *>(ws + L.sink_parts);
@@ -1413,14 +1448,18 @@ int launch_bwd(const void *q, const void *k, const void *v, const void *o, const
                int64_t T, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d, float scale,
                void *dq, void *dk, void *dv, bool accumulate, void *ws, const BwdLayout &L,
                hipStream_t st, const KernelTimer *tm_kv, const KernelTimer *tm_q, bool exact_o,
-               const Window &win) {
-  const auto launch = d == 128 ? (win.size ? launch_bwd_d<128, true> : launch_bwd_d<128, false>)
-                               : (win.size ? launch_bwd_d<64, true> : launch_bwd_d<64, false>);
+               const Window &win, const Held &q8, const Held &o8) {
+  const bool w = win.size > 0, held = q8.q != nullptr;
+  const auto launch =
+      d == 128 ? (!w ? launch_bwd_d<128, false, false>
+                     : held ? launch_bwd_d<128, true, true> : launch_bwd_d<128, true, false>)
+               : (!w ? launch_bwd_d<64, false, false>
+                     : held ? launch_bwd_d<64, true, true> : launch_bwd_d<64, true, false>);
   return launch(static_cast<const bf16 *>(q), static_cast<const bf16 *>(k),
                 static_cast<const bf16 *>(v), static_cast<const bf16 *>(o), lse,
                 static_cast<const bf16 *>(dout), cu, n, tiles, T, n_q, n_kv, h_q, h_kv, scale,
                 static_cast<bf16 *>(dq), dk, dv, accumulate, static_cast<char *>(ws), L, st, tm_kv,
-                tm_q, exact_o, win);
+                tm_q, exact_o, win, q8, o8);
 }
 
 }  // namespace libra

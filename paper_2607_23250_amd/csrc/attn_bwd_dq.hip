@@ -50,18 +50,16 @@ struct DqShape {
 // 32K pack, 64.8 to 64.6 on the 256K share.  One barrier per block; a 4-stage K / V ring (block i read by the S^T and
 // dP^T products, block i - 1 by the dQ^T products, blocks i + 1 and i + 2
 // land).
-//
-// WIN: windowed attention, with steps, masks and key rows as in the forward's.
 // d_fix: 1, or 0 where O and LSE do not belong to the given Q, K and V (8-bit
 // checkpoints): then P does not sum to 1, and D is rowsum(dO * O) for dK as for dQ.
-template <int D, bool WIN>
+template <int D>
 __global__ __launch_bounds__(2 * kThreads, 1) void attn_bwd_dq_kernel(
     const bf16 *__restrict__ q, const bf16 *__restrict__ dout, const bf16 *__restrict__ k,
     const bf16 *__restrict__ v, const float *__restrict__ stats,
     const int64_t *__restrict__ cu, const FwdItem *__restrict__ items,
     int32_t *__restrict__ hdr, int h_q, int h_kv, int64_t n_q, int64_t n_kv, int64_t nq_pad,
     float c2, float scale, bf16 *__restrict__ dq, f16 *__restrict__ rec,
-    float *__restrict__ parts, float d_fix, Window win) {
+    float *__restrict__ parts, float d_fix) {
   using S = DqShape<D>;
   extern __shared__ __attribute__((aligned(16))) bf16 smem[];
   __shared__ int32_t s_item;
@@ -97,8 +95,7 @@ __global__ __launch_bounds__(2 * kThreads, 1) void attn_bwd_dq_kernel(
 
   for (;;) {
     if (wv == 0) {
-      const int got = WIN ? take_run_item(hdr, kFwdQ, q_serve, q_state)
-                          : take_item(hdr, kFwdQ, q_serve, q_state);
+      const int got = take_item(hdr, kFwdQ, q_serve, q_state);
       if (tid == 0) s_item = got;
     }
     __syncthreads();
@@ -115,8 +112,7 @@ __global__ __launch_bounds__(2 * kThreads, 1) void attn_bwd_dq_kernel(
     const int qloc = it.q_loc0 + wrow0 + my_r;
     const int wave_qmin = it.q_loc0 + wrow0;
     const int kb0 = it.kb0, nkb = it.kb1;   // key blocks [kb0, nkb)
-    const int wave_nkb = active ? (it.q_loc0 + wrow0 + wrows - 1) / kFwdBN + 1 -
-                                      (WIN ? it.gap : 0) : 0;
+    const int wave_nkb = active ? (it.q_loc0 + wrow0 + wrows - 1) / kFwdBN + 1 : 0;
     const int pend = min(wave_nkb, nkb);    // this wave's blocks [kb0, pend)
 
     // global -> LDS, asynchronous: K and V rows of key block b (keys past the
@@ -124,24 +120,6 @@ __global__ __launch_bounds__(2 * kThreads, 1) void attn_bwd_dq_kernel(
     auto issue = [&](int b) {
       bf16 *Ks = smem + (b % S::NSTAGE) * S::STAGE;
       bf16 *Vs = Ks + S::K_EL;
-      if constexpr (WIN) {
-        const int kb = step_block(b, it.far, it.gap) * kFwdBN;
-        const int last = it.q_loc0 + it.nrows - 1 - kb;
-        const size_t off = ((size_t)(key0 + kb) * h_kv + it.g) * D;
-        const uint32_t lk = lds_addr(Ks) + 1024u * wv, lv = lds_addr(Vs) + 1024u * wv;
-        uint32_t at[S::NK];
-        static_for<S::NK>([&](auto u) {
-          const int r = swu_row<S::KC>(wv + S::NW * u, l);
-          at[u] = last >= kFwdBN - 1 ? k_lane[u]
-                                     : k_lane[u] - 2u * (uint32_t)(max(r - last, 0) * h_kv * D);
-        });
-        if constexpr (S::NK == 2)
-          g2l16x4(k + off, v + off, at[0], at[1], lk, lk + S::NW * 1024u, lv,
-                  lv + S::NW * 1024u);
-        else
-          g2l16x2(k + off, v + off, at[0], lk, lv);
-        return;
-      }
       const int kbase = key0 + b * kFwdBN;
       if (kbase + kFwdBN <= n_kv) {
         const size_t off = ((size_t)kbase * h_kv + it.g) * D;
@@ -200,8 +178,6 @@ __global__ __launch_bounds__(2 * kThreads, 1) void attn_bwd_dq_kernel(
       const bf16 *Ks = smem + (b % S::NSTAGE) * S::STAGE;   // then the V rows
       const bf16 *kp[2] = {Ks + koff[0], Ks + koff[1]};
       f32x16 sa, pa;
-      const int blk = WIN ? step_block(b, it.far, it.gap) : b;
-      const int seen = min(win.sinks, qloc + 1);   // keys below: visible sinks
       bf16x8 op[2 * NC];   // MFMA i < NC: S^T from K; NC + c: dP^T from V
       auto rd = [&](auto i) {
         constexpr int kind = i / NC, c = i % NC;
@@ -224,10 +200,8 @@ __global__ __launch_bounds__(2 * kThreads, 1) void attn_bwd_dq_kernel(
             constexpr int r = (16 / NC) * c + e;
             float x = __builtin_fmaf(sa[r], c2, neg_l2);
             if constexpr (MASK) {
-              const int kl = blk * kFwdBN + 32 * hf + 16 * (r >> 3) + 8 * kg + (r & 7);
-              const bool out = WIN ? (uint32_t)(qloc - kl) >= (uint32_t)win.size && kl >= seen
-                                   : kl > qloc;
-              x = out ? -INFINITY : x;
+              const int kl = b * kFwdBN + 32 * hf + 16 * (r >> 3) + 8 * kg + (r & 7);
+              x = kl > qloc ? -INFINITY : x;
             }
             sa[r] = fast_exp2(x);   // P^T in place
           });
@@ -280,7 +254,7 @@ __global__ __launch_bounds__(2 * kThreads, 1) void attn_bwd_dq_kernel(
     using T_ = std::true_type;
     using F_ = std::false_type;
     // blocks from (wave_qmin + 1) / 64 on reach past the wave's first row
-    const int unmasked_end = (wave_qmin + 1) / kFwdBN - (WIN ? it.gap : 0);
+    const int unmasked_end = (wave_qmin + 1) / kFwdBN;
     // iteration i: this wave's copies of block i (block i + 1's may stay in
     // flight), the barrier, then the copies of block i + 2: here for a wave
     // without a block in this iteration, else inside block() (returns true)
@@ -297,17 +271,7 @@ __global__ __launch_bounds__(2 * kThreads, 1) void attn_bwd_dq_kernel(
     int i = kb0;
     bool cp = step(i);
     if (i < pend)
-      d_run += !WIN && i < unmasked_end ? block(F_{}, F_{}, i, cp) : block(F_{}, T_{}, i, cp);
-    if constexpr (WIN) {
-      // blocks that the window of the wave's last row does not cover whole
-      const int start = wave_qmin + wrows - win.size;
-      const int masked = min(pend, max(it.far, (max(start, 0) + kFwdBN - 1) / kFwdBN - it.gap));
-      for (++i; i < masked; ++i) {
-        cp = step(i);
-        d_run += block(T_{}, T_{}, i, cp);
-      }
-      --i;
-    }
+      d_run += i < unmasked_end ? block(F_{}, F_{}, i, cp) : block(F_{}, T_{}, i, cp);
     const int pipe_end = min(pend, unmasked_end);
     // of six places modulo 32 bytes this one was the best: 64.7 ms on the 256K
     // share against 64.8 to 66.6
@@ -449,28 +413,41 @@ __global__ __launch_bounds__(256) void bwd_dq_combine_kernel(
   }
 }
 
-template <int D, bool WIN>
+template <int D>
+static void launch_combine_d(const FwdSplit *splits, const int32_t *hdr, const float *parts,
+                             const float *stats, int h_q, int64_t nq_pad, float scale, bf16 *dq,
+                             f16 *rec, float d_fix, int blocks, hipStream_t st) {
+  hipLaunchKernelGGL(bwd_dq_combine_kernel<D>, dim3(blocks), dim3(256), 0, st, splits, hdr, parts,
+                     stats, h_q, nq_pad, scale, dq, rec, d_fix);
+}
+void launch_dq_combine(int d, const FwdSplit *splits, const int32_t *hdr, const float *parts,
+                       const float *stats, int h_q, int64_t nq_pad, float scale, bf16 *dq,
+                       f16 *rec, float d_fix, int blocks, hipStream_t st) {
+  (d == 128 ? launch_combine_d<128> : launch_combine_d<64>)(splits, hdr, parts, stats, h_q, nq_pad,
+                                                            scale, dq, rec, d_fix, blocks, st);
+}
+
+template <int D>
 static int launch_dq(const bf16 *q, const bf16 *dout, const bf16 *k, const bf16 *v,
                      const float *stats, const int64_t *cu, const FwdItem *items, int32_t *hdr,
                      int h_q, int h_kv, int64_t n_q, int64_t n_kv, int64_t nq_pad, float scale,
                      bf16 *dq, f16 *rec, const FwdSplit *splits, float *parts, int max_parts,
-                     int blocks, hipStream_t st, const KernelTimer *tm, float d_fix,
-                     const Window &win) {
+                     int blocks, hipStream_t st, const KernelTimer *tm, float d_fix) {
   constexpr size_t smem = DqShape<D>::SMEM;
   static bool attr_set = false;
   if (!attr_set) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_bwd_dq_kernel<D, WIN>),
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_bwd_dq_kernel<D>),
                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != hipSuccess)
       return fail(LIBRA_EHIP, "cannot reserve %zu bytes of LDS for the dQ kernel", smem);
     attr_set = true;
   }
   if (tm) hipEventRecord(tm->begin, st);
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(attn_bwd_dq_kernel<D, WIN>), dim3(blocks), dim3(2 * kThreads),
-                     smem, st, q, dout, k, v, stats, cu, items, hdr, h_q, h_kv, n_q, n_kv, nq_pad,
-                     scale * kLog2e, scale, dq, rec, parts, d_fix, win);
+  hipLaunchKernelGGL(attn_bwd_dq_kernel<D>, dim3(blocks), dim3(2 * kThreads), smem, st, q, dout, k,
+                     v, stats, cu, items, hdr, h_q, h_kv, n_q, n_kv, nq_pad, scale * kLog2e, scale,
+                     dq, rec, parts, d_fix);
   if (max_parts > 0)
-    hipLaunchKernelGGL(bwd_dq_combine_kernel<D>, dim3(blocks * 4), dim3(256), 0, st, splits, hdr,
-                       parts, stats, h_q, nq_pad, scale, dq, rec, d_fix);
+    launch_dq_combine(D, splits, hdr, parts, stats, h_q, nq_pad, scale, dq, rec, d_fix, blocks * 4,
+                      st);
   if (tm) hipEventRecord(tm->end, st);
   return LIBRA_OK;
 }
@@ -479,12 +456,11 @@ int launch_bwd_dq(int d, const bf16 *q, const bf16 *dout, const bf16 *k, const b
                   const float *stats, const int64_t *cu, const FwdItem *items, int32_t *hdr,
                   int h_q, int h_kv, int64_t n_q, int64_t n_kv, int64_t nq_pad, float scale,
                   bf16 *dq, f16 *rec, const FwdSplit *splits, float *parts, int max_parts,
-                  int blocks, hipStream_t st, const KernelTimer *tm, float d_fix,
-                  const Window &win) {
-  const auto launch = d == 128 ? (win.size ? launch_dq<128, true> : launch_dq<128, false>)
-                               : (win.size ? launch_dq<64, true> : launch_dq<64, false>);
-  return launch(q, dout, k, v, stats, cu, items, hdr, h_q, h_kv, n_q, n_kv, nq_pad, scale, dq,
-                rec, splits, parts, max_parts, blocks, st, tm, d_fix, win);
+                  int blocks, hipStream_t st, const KernelTimer *tm, float d_fix) {
+  return (d == 128 ? launch_dq<128> : launch_dq<64>)(q, dout, k, v, stats, cu, items, hdr, h_q,
+                                                     h_kv, n_q, n_kv, nq_pad, scale, dq, rec,
+                                                     splits, parts, max_parts, blocks, st, tm,
+                                                     d_fix);
 }
 
 }  // namespace libra

@@ -250,6 +250,21 @@ struct Window {
   int32_t size = 0;    // 0: no window (plain causal attention)
   int32_t sinks = 0;
 };
+// An 8-bit checkpoint (ckpt8.hip): integers, and an exponent + 127 for each 32 of them.
+struct Held {
+  const int8_t *q = nullptr;
+  const uint8_t *e = nullptr;
+};
+// Elements [at, at + 8) of one, as bf16 (exact); at is a multiple of 8.
+__device__ __forceinline__ bf16x8 held8(const Held &x, size_t at) {
+  typedef int8_t i8x8 __attribute__((ext_vector_type(8)));
+  const i8x8 n = *reinterpret_cast<const i8x8 *>(x.q + at);
+  const uint32_t b = x.e[at >> 5];
+  const float unit = __uint_as_float(b == 255 ? 0x7fc00000u : b << 23);
+  bf16x8 r;
+  static_for<8>([&](auto i) { r[int(i)] = static_cast<bf16>((float)n[int(i)] * unit); });
+  return r;
+}
 // A sample whose rows reach this far past the window of its first key has the
 // gradients of its sink keys summed over those far rows by a kernel of their
 // own; in shorter ones the far rows are part of the sink keys' dK / dV items.
@@ -273,7 +288,7 @@ __device__ __forceinline__ int step_block(int step, int far, int gap) {
 struct FwdItem {
   int32_t q_row0;   // Q/O row of the first row
   int32_t q_loc0;   // sample-local position of the first row
-  int32_t sample;   // sample index j
+  int32_t sample;   // sample index j; windowed: the sample's first key
   int32_t head0;    // first query head
   int32_t nh;       // heads (1..4)
   int32_t nrows;    // rows (1..128)
@@ -752,13 +767,18 @@ int launch_bwd_dq(int d, const bf16 *q, const bf16 *dout, const bf16 *k, const b
                   const float *stats, const int64_t *cu, const FwdItem *items, int32_t *hdr,
                   int h_q, int h_kv, int64_t n_q, int64_t n_kv, int64_t nq_pad, float scale,
                   bf16 *dq, f16 *rec, const FwdSplit *splits, float *parts, int max_parts,
-                  int blocks, hipStream_t st, const KernelTimer *tm, float d_fix,
-                  const Window &win);
+                  int blocks, hipStream_t st, const KernelTimer *tm, float d_fix);
+// The merge of its split items' parts, on `blocks` workgroups.
+void launch_dq_combine(int d, const FwdSplit *splits, const int32_t *hdr, const float *parts,
+                       const float *stats, int h_q, int64_t nq_pad, float scale, bf16 *dq,
+                       f16 *rec, float d_fix, int blocks, hipStream_t st);
 int launch_bwd(const void *q, const void *k, const void *v, const void *o, const float *lse,
                const void *dout, const int64_t *cu, int64_t n, const libra_tile_t *tiles,
                int64_t T, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d, float scale,
                void *dq, void *dk, void *dv, bool accumulate, void *ws, const BwdLayout &L,
                hipStream_t st, const KernelTimer *tm_kv, const KernelTimer *tm_q,
-               bool exact_o = true, const Window &win = {});   // exact_o: see d_fix of dQ
+               bool exact_o = true,   // see d_fix of the dQ kernel
+               const Window &win = {},
+               const Held &q8 = {}, const Held &o8 = {});   // windowed: q and o, if q and o are null
 
 }  // namespace libra

@@ -165,7 +165,7 @@ __global__ __launch_bounds__(kThreads, kFwdPerCu<D>) void attn_fwd_kernel(
     const int idx = __builtin_amdgcn_readfirstlane(s_item);
     if (idx < 0) break;
     const FwdItem it = items[idx];
-    const int64_t key0 = cu[it.sample];
+    const int64_t key0 = WIN ? (int64_t)it.sample : cu[it.sample];
     const int head = it.head0 + (w % it.nh);
     const int wrow0 = (w / it.nh) * kRows;
     const int wrows = min(max(it.nrows - wrow0, 0), kRows);

@@ -85,7 +85,8 @@ __device__ __forceinline__ void head_chunk(int hb, int he, int G, int c, int &g,
 }
 
 // The items of one head chunk whose first row lies in rows [wa, wb) of a tile
-// (at most 32 rows): f(item), with its steps in kb1.
+// (at most 32 rows): f(item), with its steps in kb1 and, in the place of the sample's index,
+// its first key.
 template <typename F>
 __device__ __forceinline__ void for_each_win_item(const libra_tile_t &t, int64_t wa, int64_t wb,
                                                   const CuView &cu, int64_t n, int g, int h0,
@@ -104,7 +105,7 @@ __device__ __forceinline__ void for_each_win_item(const libra_tile_t &t, int64_t
       const int32_t qmin = (int32_t)(pb + rb - c0), qmax = qmin + nrows - 1;
       const int w0 = max(0, qmin - win.size + 1) / kFwdBN;   // first block of the window
       const int far = min((win.sinks + kFwdBN - 1) / kFwdBN, w0);
-      f(FwdItem{(int32_t)(t.q_row + (pb + rb - t.q_begin)), qmin, (int32_t)j, h0, nh, nrows, g, 0,
+      f(FwdItem{(int32_t)(t.q_row + (pb + rb - t.q_begin)), qmin, (int32_t)c0, h0, nh, nrows, g, 0,
                 far + qmax / kFwdBN + 1 - w0, -1, far, w0 - far});
     }
   }
@@ -372,6 +373,24 @@ inline bool win_may_split(const Window &w, int64_t n_kv) {
   return (reach < n_kv ? reach : n_kv) / kFwdBN + 1 + (w.sinks + kFwdBN - 1) / kFwdBN >=
          2 * kWinMinSteps;
 }
+
+// Arguments of the windowed dQ kernel (attn_window_dq.hip).  q and o, or q8 and o8.
+struct WinDq {
+  const bf16 *q, *o, *dout, *k, *v;
+  Held q8, o8;
+  const float *lse;
+  const FwdItem *items;
+  int32_t *hdr;
+  int h_q, h_kv;
+  int64_t n_q, nq_pad;
+  float scale, c2, d_fix;   // d_fix: see attn_bwd_dq.hip
+  Window win;
+  bf16 *dq;
+  f16 *rec;
+  float *stats, *parts;
+};
+constexpr int kWinDqPerCu = 2;   // workgroups per CU
+int launch_win_dq(int d, const WinDq &a, int cus, hipStream_t st);
 
 // Launchers (attn_window.hip).
 void launch_win_prep_fwd(const WinPrep &p, hipStream_t st);

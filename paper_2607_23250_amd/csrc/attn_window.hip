@@ -249,16 +249,18 @@ void launch_win_prep_bwd(const WinPrep &q, const WinBwdPrep &b, int grid_kv, hip
 // ---------------------------------------------------------------------------
 // dK and dV of 32 sink keys of a KV head, over a range of the sample's far rows.  The
 // products are those of the dK / dV kernel (queries on M, this lane's key on N); each wave
-// holds all 32 keys and takes every fourth step (32 rows x two heads) through an LDS stage
-// of its own, so that no wave waits for another until the four sums are added up.  Bound by
-// the records it reads: with few sinks, one of the 32 columns in eight or so counts.
+// holds all 32 keys and takes every fourth step (32 rows x two heads), head by head, through
+// two LDS stages of its own, so that no wave waits for another until the four sums are
+// added up.  Bound by the records it reads: with few sinks, one of the 32 columns in eight or
+// so counts.
 template <int D>
 __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 1))) void
 win_sink_kernel(const f16 *__restrict__ k, const f16 *__restrict__ v,
                 const f16 *__restrict__ rec, WinBwdPrep a, float c2,
                 float *__restrict__ parts) {
   using S = KvShape<D>;
-  constexpr int NC = D / 16, NT = D / 32;
+  constexpr int NC = D / 16, NT = D / 32, LOADS = S::HEAD_EL / 512;   // LOADS: KiB of a record
+  static_assert(LOADS <= 63, "vmcnt range");
   extern __shared__ __attribute__((aligned(16))) bf16 smem[];
   const int tid = threadIdx.x, l = tid & 63, ln = l & 31, kg = l >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -296,6 +298,7 @@ win_sink_kernel(const f16 *__restrict__ k, const f16 *__restrict__ v,
         vf[c] = *reinterpret_cast<const f16x8 *>(v + off);
       }
     });
+    wait_vm_known();
     f32x16 dva[NT], dka[NT];
     static_for<NT>([&](auto dt) {
       dva[dt] = mfma_zero_c();
@@ -304,51 +307,77 @@ win_sink_kernel(const f16 *__restrict__ k, const f16 *__restrict__ v,
     StepIter it{a.tiles, (int64_t)item.t1 + 1, a.n_q, a.n_kv, key0, key0 + item.r0,
                 key0 + item.r1, a.h_q, item.g, G, 0, 2 * S::HEAD_EL / 1024};
     it.start(item.t0);
-    for (int n = 0; it.valid; ++n, it.next()) {
-      if ((n & (kWaves - 1)) != w) continue;
-      // the records of heads h and h + 1 (the one after a last odd head is not used)
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the stage's reads are done
-      const char *src = reinterpret_cast<const char *>(rec) + (uniform64(it.rec) << 10);
-      static_for<S::STAGE_EL / 512 / 4>([&](auto i) {
-        g2l_run<4>(src + 4096 * i, 16u * l, stage_at + 4096u * i);
-      });
-      wait_vm();
-      const int qb = it.qb(), lo = it.lo();
-      const int first = kl + a.win.size - qb;   // first row of the block past the window
-      const int lower = max(lo, min(first, kRows)) - 8 * kg;
-      const int upper = (key_ok ? it.hi() : 0) - 8 * kg;
-      const int heads = it.two() ? 2 : 1;
-      for (int hb = 0; hb < heads; ++hb) {
-        const bf16 *Qs = stage + hb * S::HEAD_EL;
-        const bf16 *Ag = Qs + 2 * S::Q_EL + 8 * l;
-        const bf16 *rp[2] = {Qs + qoff[0], Qs + qoff[1]};
-        const f16 *tp[2] = {reinterpret_cast<const f16 *>(Qs) + troff[0],
-                            reinterpret_cast<const f16 *>(Qs) + troff[1]};
-        f32x16 sa = mfma32h(*reinterpret_cast<const f16x8 *>(Ag), ones3, mfma_zero_c());
-        f32x16 pa =
-            mfma32h(*reinterpret_cast<const f16x8 *>(Ag + kAugEl / 2), ones3, mfma_zero_c());
-        static_for<NC>([&](auto c) {
-          sa = mfma32h(*reinterpret_cast<const f16x8 *>(rp[c & 1] + 1024 * (c >> 1)), kf[c], sa);
-          pa = mfma32h(*reinterpret_cast<const f16x8 *>(rp[c & 1] + S::Q_EL + 1024 * (c >> 1)),
-                       vf[c], pa);
-        });
-        f16x8 p16[2], s16[2];
-        static_for<16>([&](auto r) {
-          constexpr int iq = 16 * (r >> 3) + (r & 7);
-          const float x = iq >= lower && iq < upper ? sa[int(r)] * c2s : -INFINITY;
-          const float p = fast_exp2(x);
-          p16[r >> 3][r & 7] = static_cast<f16>(p);
-          s16[r >> 3][r & 7] = static_cast<f16>(p * pa[int(r)]);
-        });
-        static_for<NT>([&](auto dt) {
-          static_for<2>([&](auto c) {
-            constexpr int at = 128 * c + 1024 * dt;
-            dva[dt] = mfma32h(lds_tr16x2h(tp[0] + S::Q_EL + at, tp[1] + S::Q_EL + at), p16[c],
-                              dva[dt]);
-            dka[dt] = mfma32h(lds_tr16x2h(tp[0] + at, tp[1] + at), s16[c], dka[dt]);
-          });
-        });
+    // this wave's units: the heads of every fourth step, the copy of the next one under way
+    // while one is computed
+    int n = 0, hb = 0;
+    auto skip = [&]() {   // to the next step of this wave
+      for (; it.valid && (n & (kWaves - 1)) != w; ++n) it.next();
+    };
+    struct Unit {
+      int lower, upper;   // rows of the block that count for this lane's key, less 8 kg
+    };
+    auto copy = [&](int buf) {
+      const int qb = it.qb(), first = kl + a.win.size - qb;   // first row past the window
+      const Unit u{max(it.lo(), min(first, kRows)) - 8 * kg, (key_ok ? it.hi() : 0) - 8 * kg};
+      const char *src = reinterpret_cast<const char *>(rec) +
+                        (uniform64(it.rec + hb * (S::HEAD_EL / 512)) << 10);
+      const uint32_t dst = stage_at + (uint32_t)(buf * S::HEAD_EL * sizeof(bf16));
+      static_for<LOADS / 4>([&](auto i) { g2l_run<4>(src + 4096 * i, 16u * l, dst + 4096u * i); });
+      if constexpr (LOADS % 4 != 0)
+        g2l_run<LOADS % 4>(src + LOADS / 4 * 4096, 16u * l, dst + LOADS / 4 * 4096u);
+      if (hb == 0 && it.two()) {
+        hb = 1;
+      } else {
+        hb = 0;
+        it.next();
+        ++n;
+        skip();
       }
+      return u;
+    };
+    skip();
+    bool more = it.valid;
+    Unit next{};
+    if (more) next = copy(0);
+    for (int buf = 0; more; buf ^= 1) {
+      const Unit u = next;
+      more = it.valid;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the other stage's reads are done
+      if (more) {
+        next = copy(buf ^ 1);
+        wait_vm_n<LOADS>();
+      } else {
+        wait_vm();
+      }
+      const bf16 *Qs = stage + buf * S::HEAD_EL;
+      const bf16 *Ag = Qs + 2 * S::Q_EL + 8 * l;
+      const bf16 *rp[2] = {Qs + qoff[0], Qs + qoff[1]};
+      const f16 *tp[2] = {reinterpret_cast<const f16 *>(Qs) + troff[0],
+                          reinterpret_cast<const f16 *>(Qs) + troff[1]};
+      f32x16 sa = mfma32h(*reinterpret_cast<const f16x8 *>(Ag), ones3, mfma_zero_c());
+      f32x16 pa =
+          mfma32h(*reinterpret_cast<const f16x8 *>(Ag + kAugEl / 2), ones3, mfma_zero_c());
+      static_for<NC>([&](auto c) {
+        sa = mfma32h(*reinterpret_cast<const f16x8 *>(rp[c & 1] + 1024 * (c >> 1)), kf[c], sa);
+        pa = mfma32h(*reinterpret_cast<const f16x8 *>(rp[c & 1] + S::Q_EL + 1024 * (c >> 1)),
+                     vf[c], pa);
+      });
+      f16x8 p16[2], s16[2];
+      static_for<16>([&](auto r) {
+        constexpr int iq = 16 * (r >> 3) + (r & 7);
+        const float x = iq >= u.lower && iq < u.upper ? sa[int(r)] * c2s : -INFINITY;
+        const float p = fast_exp2(x);
+        p16[r >> 3][r & 7] = static_cast<f16>(p);
+        s16[r >> 3][r & 7] = static_cast<f16>(p * pa[int(r)]);
+      });
+      static_for<NT>([&](auto dt) {
+        static_for<2>([&](auto c) {
+          constexpr int at = 128 * c + 1024 * dt;
+          dva[dt] = mfma32h(lds_tr16x2h(tp[0] + S::Q_EL + at, tp[1] + S::Q_EL + at), p16[c],
+                            dva[dt]);
+          dka[dt] = mfma32h(lds_tr16x2h(tp[0] + at, tp[1] + at), s16[c], dka[dt]);
+        });
+      });
     }
     // the waves' sums, each in its own stage, then added in wave order
     static_assert(2 * NT * 16 * 64 * sizeof(float) <= S::STAGE_EL * sizeof(bf16), "fits");
