@@ -9,6 +9,7 @@ and a missing library raises immediately.
 from __future__ import annotations
 
 import array
+import contextlib
 import ctypes
 import itertools
 import os
@@ -279,7 +280,20 @@ def _dptr(t) -> Optional[int]:
 
 def _stream(device):
     torch = _torch()
+    # the stream's handle alone where torch hands it out (0.1 us; a Stream object takes 1.8,
+    # as long as a small kernel)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is not None and device.index is not None:
+        return ctypes.c_void_p(raw(device.index))
     return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+
+
+def _on(device):
+    """Makes ``device`` the current one for a ``with`` block, if it is not."""
+    torch = _torch()
+    if torch.cuda.current_device() == device.index:
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
 
 
 def _need(t, dtype, shape, name):
@@ -449,7 +463,7 @@ def libra_attn_window_fwd(q, k, v, cu_seqlens, tiles, *, window: int, sinks: int
     workspace = _workspace(workspace, 0 if workspace is not None else
                            libra_attn_window_workspace_size(*sizes, False, window=window,
                                                             sinks=sinks), q.device)
-    with torch.cuda.device(q.device):
+    with _on(q.device):
         _check(lib().libra_attn_window_fwd(
             q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_seqlens.data_ptr(), n, tiles.data_ptr(),
             T, n_q, n_kv, h_q, h_kv, d, window, sinks, softmax_scale, o.data_ptr(),
@@ -496,7 +510,7 @@ def libra_attn_window_bwd(q, k, v, o, lse, dout, cu_seqlens, tiles, *, window: i
     workspace = _workspace(workspace, 0 if workspace is not None else
                            libra_attn_window_workspace_size(*sizes, True, window=window,
                                                             sinks=sinks), q.device)
-    with torch.cuda.device(q.device):
+    with _on(q.device):
         _check(lib().libra_attn_window_bwd(
             q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
             dout.data_ptr(), cu_seqlens.data_ptr(), n, tiles.data_ptr(), T, n_q, n_kv, h_q, h_kv,
@@ -550,7 +564,7 @@ def libra_ckpt8_pack(x, *, q=None, e=None):
     _need(q, torch.int8, x.shape, "q")
     _need(e, torch.uint8, e_shape, "e")
     _same_device(x, (q, "q"), (e, "e"))
-    with torch.cuda.device(x.device):
+    with _on(x.device):
         _check(lib().libra_ckpt8_pack(x.data_ptr(), dtype, rows, cols, ld, q.data_ptr(),
                                       e.data_ptr(), _stream(x.device)), "libra_ckpt8_pack")
     return q, e
@@ -573,7 +587,7 @@ def libra_ckpt8_unpack(q, e, *, dtype=None, out=None):
         raise ValueError(f"out: need shape {tuple(q.shape)}, got {tuple(out.shape)}")
     _same_device(q, (e, "e"), (out, "out"))
     rows, cols, ld = _rows_cols_ld(out, "out")
-    with torch.cuda.device(q.device):
+    with _on(q.device):
         _check(lib().libra_ckpt8_unpack(q.data_ptr(), e.data_ptr(), rows, cols, kind, ld,
                                         out.data_ptr(), _stream(q.device)), "libra_ckpt8_unpack")
     return out
@@ -610,7 +624,7 @@ def libra_attn_bwd_ckpt8(q, k, v, o, lse, dout, cu_seqlens, tiles, *, window: in
                            libra_attn_bwd_ckpt8_workspace_size(*sizes, window=window,
                                                                sinks=sinks), ref.device)
     c = [ctypes.byref(_Ckpt8(x.data_ptr(), e.data_ptr())) for x, e in held]
-    with torch.cuda.device(ref.device):
+    with _on(ref.device):
         _check(lib().libra_attn_bwd_ckpt8(
             *c, lse.data_ptr(), dout.data_ptr(), cu_seqlens.data_ptr(), n, tiles.data_ptr(), T,
             n_q, n_kv, h_q, h_kv, d, window, sinks, softmax_scale, dq.data_ptr(), dk.data_ptr(),

@@ -19,7 +19,7 @@ OUT_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "liblibra.so")
 
 HIP_SOURCES = ["attn_fwd.hip", "attn_bwd.hip", "attn_bwd_dq.hip", "attn_window.hip",
-               "attn_window_dq.hip", "attn_api.hip", "ckpt8.hip", "mfma_loop.hip"]
+               "attn_window_fwd.hip", "attn_window_dq.hip", "attn_api.hip", "ckpt8.hip", "mfma_loop.hip"]
 CXX_SOURCES = ["plan.cpp", "vrsp.cpp"]
 ARCH = os.environ.get("LIBRA_OFFLOAD_ARCH", "gfx950")
 
@@ -31,7 +31,7 @@ def _hipcc() -> str:
     raise RuntimeError("hipcc not found")
 
 
-# Per-source extra flags.  The forward and dK / dV kernels take the MFMA
+# Per-source extra flags.  The forward, dK / dV and windowed kernels take the MFMA
 # results that the VALU reads (S, dP) in VGPRs; the default heuristic lands
 # them in AGPRs and copies every element out before use.  The compiler still
 # keeps the long-lived dK / dV accumulators in AGPRs.  The dQ kernel stays in
@@ -42,6 +42,8 @@ EXTRA_FLAGS = {
     "attn_api.hip": _VGPR_FORM,
     "attn_bwd.hip": _VGPR_FORM,
     "attn_window.hip": _VGPR_FORM,
+    "attn_window_fwd.hip": _VGPR_FORM,
+    "attn_window_dq.hip": _VGPR_FORM,
 }
 
 

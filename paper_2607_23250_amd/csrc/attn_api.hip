@@ -167,9 +167,12 @@ int attn_fwd(const void *q, const void *k, const void *v, const int64_t *cu_seql
   int rc = LIBRA_OK;
   const KernelTimer *tm = next_timer(0, &rc);
   if (rc) return rc;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  if (win.size)
+    return launch_win_fwd(q, k, v, cu_seqlens, num_samples, tiles, num_tiles, n_q_rows, n_kv_rows,
+                          h_q, h_kv, head_dim, scale, o, lse, workspace, L, st, tm, win);
   return launch_fwd(q, k, v, cu_seqlens, num_samples, tiles, num_tiles, n_q_rows, n_kv_rows, h_q,
-                    h_kv, head_dim, scale, o, lse, workspace, L,
-                    static_cast<hipStream_t>(stream), tm, win);
+                    h_kv, head_dim, scale, o, lse, workspace, L, st, tm);
 }
 
 // The checks of a backward call that come before its workspace's.

@@ -1067,7 +1067,7 @@ __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 
     // Steps are walked once, at issue; what the compute side needs of the step
     // in ring stage j (lo | hi << 8 | two << 16, and the q_loc of the block's
     // row 0) waits in lane j of desc / desc_qb.
-    StepIter iss{tiles, WIN ? (int64_t)item.t1 + 1 : T, n_q, n_kv, key0, key0 + item.r0,
+    StepIter<WIN> iss{tiles, WIN ? (int64_t)item.t1 + 1 : T, n_q, n_kv, key0, key0 + item.r0,
                  key0 + (item.r1 < len ? item.r1 : len), h_q, g, G, kloc0, 2 * S::HEAD_EL / 1024};
     iss.start(WIN ? item.t0 : 0);
     int desc = 0, desc_qb = 0;

@@ -39,6 +39,12 @@ struct KvShape {
 // fragment (one tile's rows of the sample) everything a step needs is
 // precomputed, so that advancing is a few 32-bit scalar operations plus one
 // running 64-bit record offset.
+//
+// LANES: the lanes of the wave look at 64 tiles at once for the next one with rows of the
+// item.  A windowed item meets few of its candidates, and one tile after another cost up
+// to 0.5 us each (the far rows of a 16K sample, 16 tiles x 2 head shards: 159 us, [SINK] with
+// this search).
+template <bool LANES>
 struct StepIter {
   const libra_tile_t *tiles;
   int64_t T, n_q, n_kv, key0, p0, p1;   // rows at positions [p0, p1)
@@ -52,7 +58,25 @@ struct StepIter {
   int64_t rec;              // offset of the record of (block, h), in KiB
   bool valid;
 
+  // the first tile from `from` on with rows of the item (T: none)
+  __device__ int64_t find(int64_t from) const {
+    const int lane = threadIdx.x & 63;
+    for (; from < T; from += 64) {
+      bool has = false;
+      if (from + lane < T) {
+        const libra_tile_t tl = tiles[from + lane];
+        const int64_t pb = tl.q_begin > p0 ? tl.q_begin : p0;
+        const int64_t pe = tl.q_end < p1 ? tl.q_end : p1;
+        has = tile_ok(tl, n_q, n_kv, h_q) && pb < pe && pe > key0 + kloc0 &&
+              tl.head_begin < (g + 1) * G && tl.head_end > g * G;
+      }
+      const unsigned long long m = __builtin_amdgcn_ballot_w64(has);
+      if (m) return from + __builtin_ctzll(m);
+    }
+    return T;
+  }
   __device__ bool seek() {
+    if constexpr (LANES) t = find(t);
     for (; t < T; ++t) {
       const libra_tile_t tl = tiles[t];
       if (!tile_ok(tl, n_q, n_kv, h_q)) continue;

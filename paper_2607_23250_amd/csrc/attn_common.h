@@ -759,8 +759,15 @@ int64_t fwd_max_items(int64_t T, int64_t n, int64_t n_q, int h_q, int h_kv);
 int launch_fwd(const void *q, const void *k, const void *v, const int64_t *cu, int64_t n,
                const libra_tile_t *tiles, int64_t T, int64_t n_q, int64_t n_kv, int h_q,
                int h_kv, int d, float scale, void *o, float *lse, void *ws,
-               const FwdLayout &L, hipStream_t st, const KernelTimer *tm,
-               const Window &win = {});
+               const FwdLayout &L, hipStream_t st, const KernelTimer *tm);
+// The merge of its split items' parts, on `blocks` workgroups.
+void launch_fwd_combine(int d, const FwdSplit *splits, const int32_t *hdr, const float *parts,
+                        int h_q, int64_t n_q, bf16 *o, float *lse, int blocks, hipStream_t st);
+// The windowed forward (attn_window_fwd.hip).
+int launch_win_fwd(const void *q, const void *k, const void *v, const int64_t *cu, int64_t n,
+                   const libra_tile_t *tiles, int64_t T, int64_t n_q, int64_t n_kv, int h_q,
+                   int h_kv, int d, float scale, void *o, float *lse, void *ws,
+                   const FwdLayout &L, hipStream_t st, const KernelTimer *tm, const Window &win);
 // The dQ kernel of the backward pass (attn_bwd_dq.hip), on `blocks`
 // persistent workgroups over the forward-style work items.
 int launch_bwd_dq(int d, const bf16 *q, const bf16 *dout, const bf16 *k, const bf16 *v,

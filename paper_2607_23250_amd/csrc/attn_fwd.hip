@@ -23,7 +23,6 @@
 
 #include "attn_common.h"
 #include "attn_items.h"
-#include "attn_win_items.h"
 #include "errors.h"
 
 namespace libra {
@@ -98,6 +97,16 @@ __global__ __launch_bounds__(256) void fwd_combine_kernel(
   }
 }
 
+void launch_fwd_combine(int d, const FwdSplit *splits, const int32_t *hdr, const float *parts,
+                        int h_q, int64_t n_q, bf16 *o, float *lse, int blocks, hipStream_t st) {
+  if (d == 128)
+    hipLaunchKernelGGL(fwd_combine_kernel<128>, dim3(blocks), dim3(256), 0, st, splits, hdr, parts,
+                       h_q, n_q, o, lse);
+  else
+    hipLaunchKernelGGL(fwd_combine_kernel<64>, dim3(blocks), dim3(256), 0, st, splits, hdr, parts,
+                       h_q, n_q, o, lse);
+}
+
 // ---------------------------------------------------------------------------
 template <int D>
 struct FwdShape {
@@ -114,17 +123,12 @@ struct FwdShape {
 template <int D>
 constexpr int kFwdPerCu = D == 64 ? 3 : 2;
 
-//
-// WIN: windowed attention.  The item's key blocks are steps (step_block); a block
-// that some row's window does not cover whole is masked by element; a block may hold
-// no key of a row, so the running max starts at the lowest finite value; and keys past
-// the item's last row are not read (in a cache they may hold anything).
-template <int D, bool WIN>
+template <int D>
 __global__ __launch_bounds__(kThreads, kFwdPerCu<D>) void attn_fwd_kernel(
     const bf16 *__restrict__ q, const bf16 *__restrict__ k, const bf16 *__restrict__ v,
     const int64_t *__restrict__ cu, const FwdItem *__restrict__ items, int32_t *__restrict__ hdr,
     int h_q, int h_kv, int64_t n_q, int64_t n_kv, float c2,
-    bf16 *__restrict__ o, float *__restrict__ lse, float *__restrict__ parts, Window win) {
+    bf16 *__restrict__ o, float *__restrict__ lse, float *__restrict__ parts) {
   using S = FwdShape<D>;
   extern __shared__ __attribute__((aligned(16))) bf16 smem[];
   __shared__ int32_t s_item;
@@ -157,15 +161,14 @@ __global__ __launch_bounds__(kThreads, kFwdPerCu<D>) void attn_fwd_kernel(
 
   for (;;) {
     if (w == 0) {
-      const int got = WIN ? take_run_item(hdr, kFwdQ, q_serve, q_state)
-                          : take_item(hdr, kFwdQ, q_serve, q_state);
+      const int got = take_item(hdr, kFwdQ, q_serve, q_state);
       if (tid == 0) s_item = got;
     }
     __syncthreads();
     const int idx = __builtin_amdgcn_readfirstlane(s_item);
     if (idx < 0) break;
     const FwdItem it = items[idx];
-    const int64_t key0 = WIN ? (int64_t)it.sample : cu[it.sample];
+    const int64_t key0 = cu[it.sample];
     const int head = it.head0 + (w % it.nh);
     const int wrow0 = (w / it.nh) * kRows;
     const int wrows = min(max(it.nrows - wrow0, 0), kRows);
@@ -175,8 +178,7 @@ __global__ __launch_bounds__(kThreads, kFwdPerCu<D>) void attn_fwd_kernel(
     const int qloc = it.q_loc0 + wrow0 + my_r;
     const int wave_qmin = it.q_loc0 + wrow0;
     const int kb0 = it.kb0, nkb = it.kb1;   // key blocks [kb0, nkb)
-    int wave_nkb = active ? (it.q_loc0 + wrow0 + wrows - 1) / kFwdBN + 1 : 0;
-    if constexpr (WIN) wave_nkb -= active ? it.gap : 0;   // a step, like kb0 and nkb
+    const int wave_nkb = active ? (it.q_loc0 + wrow0 + wrows - 1) / kFwdBN + 1 : 0;
 
     bf16x8 qf[D / 16];
     if (active) {
@@ -193,30 +195,6 @@ __global__ __launch_bounds__(kThreads, kFwdPerCu<D>) void attn_fwd_kernel(
     auto issue = [&](int b, int buf, int part) {
       const bf16 *src = part ? v : k;
       bf16 *dst = smem + buf * S::STAGE + part * S::K_EL;
-      if constexpr (WIN) {
-        // keys past the item's last row read that row's key instead; the rows of a
-        // block lie less than 2^31 bytes apart (checked at the boundary)
-        const int kb = step_block(b, it.far, it.gap) * kFwdBN;
-        const int last = it.q_loc0 + it.nrows - 1 - kb;
-        const bf16 *base = src + ((size_t)(key0 + kb) * h_kv + it.g) * D;
-        const uint32_t ld = lds_addr(dst) + 1024u * w;
-        uint32_t at[S::NK];
-        static_for<S::NK>([&](auto u) {
-          const int r = swu_row<S::KC>(w + kWaves * u, l);
-          at[u] = last >= kFwdBN - 1 ? k_lane[u]
-                                     : k_lane[u] - 2u * (uint32_t)(max(r - last, 0) * h_kv * D);
-        });
-        static_for<S::NK / 4>([&](auto h) {
-          constexpr uint32_t d = 4 * h * kWaves * 1024u, e = kWaves * 1024u;
-          g2l16x4r(base, at[4 * h], at[4 * h + 1], at[4 * h + 2], at[4 * h + 3], ld + d,
-                   ld + d + e, ld + d + 2 * e, ld + d + 3 * e);
-        });
-        static_for<S::NK % 4>([&](auto i) {
-          constexpr int u = S::NK / 4 * 4 + i;
-          g2l16s(base, at[u], ld + u * kWaves * 1024u);
-        });
-        return;
-      }
       const int64_t kbase = key0 + (int64_t)b * kFwdBN;
       if (kbase + kFwdBN <= n_kv) {
         // whole block inside the buffer: one SGPR base, fixed per-lane offsets;
@@ -255,17 +233,11 @@ __global__ __launch_bounds__(kThreads, kFwdPerCu<D>) void attn_fwd_kernel(
       // cores busy while this one waits to issue; waves without rows in this
       // block post both at once)
       const bool more = b + 1 < nkb;
-      const int blk = WIN ? step_block(b, it.far, it.gap) : b;
-      bool mine = b < wave_nkb;
-      // a block before the window of the wave's first row, without sinks
-      if constexpr (WIN)
-        mine = mine && (blk * kFwdBN + kFwdBN - 1 > wave_qmin - win.size ||
-                        blk * kFwdBN < win.sinks);
-      if (!mine && more) {
+      if (b >= wave_nkb && more) {
         issue(b + 1, buf ^ 1, 0);
         issue(b + 1, buf ^ 1, 1);
       }
-      if (mine) {
+      if (b < wave_nkb) {
         constexpr int NC = D / 16, NT = D / 32, AHEAD = 4;
         const bf16 *Ks = smem + buf * S::STAGE;
         const bf16 *Vs = Ks + S::K_EL;
@@ -294,21 +266,7 @@ __global__ __launch_bounds__(kThreads, kFwdPerCu<D>) void attn_fwd_kernel(
         if (more) issue(b + 1, buf ^ 1, 0);
         // keys past the row are masked only in blocks that reach past the
         // wave's first row (the diagonal block of each row)
-        if constexpr (WIN) {
-          // the wave's last row starts its window after the block's first key, or its
-          // first row comes before the block's last
-          if (blk * kFwdBN <= wave_qmin + wrows - 1 - win.size ||
-              blk * kFwdBN + kFwdBN - 1 > wave_qmin) {
-            const int seen = min(win.sinks, qloc + 1);   // keys below: visible sinks
-            static_for<2>([&](auto t) {
-              static_for<16>([&](auto r) {
-                const int kl = blk * kFwdBN + 32 * t + 16 * (r >> 3) + 8 * kg + (r & 7);
-                if ((uint32_t)(qloc - kl) >= (uint32_t)win.size && kl >= seen)
-                  s[t][int(r)] = -INFINITY;
-              });
-            });
-          }
-        } else if (b * kFwdBN + kFwdBN - 1 > wave_qmin) {
+        if (b * kFwdBN + kFwdBN - 1 > wave_qmin) {
           static_for<2>([&](auto t) {
             static_for<16>([&](auto r) {
               const int kl = b * kFwdBN + 32 * t + 16 * (r >> 3) + 8 * kg + (r & 7);
@@ -344,7 +302,6 @@ __global__ __launch_bounds__(kThreads, kFwdPerCu<D>) void attn_fwd_kernel(
             static_for<16>([&](auto r) { mx = fmaxf(mx, s[t][int(r)]); });
           });
           mx = row_max2(mx) * c2;
-          if constexpr (WIN) mx = fmaxf(mx, -3.402823466e38f);   // a row may have no key here
           const float alpha = move ? fast_exp2(m_run - mx) : 1.f;
           m_run = move ? mx : m_run;
           l_run *= alpha;
@@ -445,19 +402,18 @@ FwdLayout fwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, i
   return L;
 }
 
-template <int D, bool WIN>
+template <int D>
 static int launch_fwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const int64_t *cu,
                         int64_t n, const libra_tile_t *tiles, int64_t T, int64_t n_q,
                         int64_t n_kv, int h_q, int h_kv, float scale, bf16 *o, float *lse,
-                        char *ws, const FwdLayout &L, hipStream_t st, const KernelTimer *tm,
-                        const Window &win) {
+                        char *ws, const FwdLayout &L, hipStream_t st, const KernelTimer *tm) {
   int32_t *hdr = reinterpret_cast<int32_t *>(ws + L.hdr);
   FwdItem *items = reinterpret_cast<FwdItem *>(ws + L.items);
   auto *splits = reinterpret_cast<FwdSplit *>(ws + L.splits);
   float *parts = reinterpret_cast<float *>(ws + L.parts);
   static bool attr_set = false;
   if (!attr_set) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_fwd_kernel<D, WIN>),
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_fwd_kernel<D>),
                             hipFuncAttributeMaxDynamicSharedMemorySize,
                             (int)FwdShape<D>::SMEM) != hipSuccess)
       return fail(LIBRA_EHIP, "hipFuncSetAttribute failed");
@@ -467,24 +423,16 @@ static int launch_fwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const int64
   hipGetDevice(&dev);
   hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
   const int grid = cus * kFwdPerCu<D>;
-  int max_parts;
-  if constexpr (WIN) {
-    max_parts = win_may_split(win, n_kv) ? L.max_parts : 0;
-    launch_win_prep_fwd(WinPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, win, hdr, items,
-                                L.max_items, 1, grid, cus * 2, max_parts, 0, splits}, st);
-  } else {
-    max_parts = may_split(n_kv) ? L.max_parts : 0;
-    hipLaunchKernelGGL(prep_fwd_kernel, dim3(1), dim3(kPrepThreads), 0, st,
-                       FwdPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, hdr, items, L.max_items, 1,
-                               grid, cus * 2, max_parts, 0, splits});
-  }
+  const int max_parts = may_split(n_kv) ? L.max_parts : 0;
+  hipLaunchKernelGGL(prep_fwd_kernel, dim3(1), dim3(kPrepThreads), 0, st,
+                     FwdPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, hdr, items, L.max_items, 1,
+                             grid, cus * 2, max_parts, 0, splits});
   if (tm) hipEventRecord(tm->begin, st);
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(attn_fwd_kernel<D, WIN>), dim3(grid), dim3(kThreads),
-                     FwdShape<D>::SMEM, st, q, k, v, cu, items, hdr, h_q, h_kv, n_q, n_kv,
-                     scale * kLog2e, o, lse, parts, win);
+  hipLaunchKernelGGL(attn_fwd_kernel<D>, dim3(grid), dim3(kThreads), FwdShape<D>::SMEM, st, q,
+                     k, v, cu, items, hdr, h_q, h_kv, n_q, n_kv, scale * kLog2e, o,
+                     lse, parts);
   if (max_parts > 0)
-    hipLaunchKernelGGL(fwd_combine_kernel<D>, dim3(cus * 4), dim3(256), 0, st, splits, hdr, parts,
-                       h_q, n_q, o, lse);
+    launch_fwd_combine(D, splits, hdr, parts, h_q, n_q, o, lse, cus * 4, st);
   if (tm) hipEventRecord(tm->end, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(LIBRA_EHIP, "forward launch failed: %s", hipGetErrorString(e));
@@ -494,12 +442,17 @@ static int launch_fwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const int64
 int launch_fwd(const void *q, const void *k, const void *v, const int64_t *cu, int64_t n,
                const libra_tile_t *tiles, int64_t T, int64_t n_q, int64_t n_kv, int h_q,
                int h_kv, int d, float scale, void *o, float *lse, void *ws,
-               const FwdLayout &L, hipStream_t st, const KernelTimer *tm, const Window &win) {
-  const auto launch = d == 128 ? (win.size ? launch_fwd_d<128, true> : launch_fwd_d<128, false>)
-                               : (win.size ? launch_fwd_d<64, true> : launch_fwd_d<64, false>);
-  return launch(static_cast<const bf16 *>(q), static_cast<const bf16 *>(k),
-                static_cast<const bf16 *>(v), cu, n, tiles, T, n_q, n_kv, h_q, h_kv, scale,
-                static_cast<bf16 *>(o), lse, static_cast<char *>(ws), L, st, tm, win);
+               const FwdLayout &L, hipStream_t st, const KernelTimer *tm) {
+  auto Q = static_cast<const bf16 *>(q);
+  auto K = static_cast<const bf16 *>(k);
+  auto V = static_cast<const bf16 *>(v);
+  auto O = static_cast<bf16 *>(o);
+  char *W = static_cast<char *>(ws);
+  if (d == 128)
+    return launch_fwd_d<128>(Q, K, V, cu, n, tiles, T, n_q, n_kv, h_q, h_kv, scale, O, lse, W, L,
+                             st, tm);
+  return launch_fwd_d<64>(Q, K, V, cu, n, tiles, T, n_q, n_kv, h_q, h_kv, scale, O, lse, W, L, st,
+                          tm);
 }
 
 }  // namespace libra

@@ -10,6 +10,19 @@
 
 namespace libra {
 
+// A record that no store of the kernel changes, at an address that is the same in every lane:
+// a scalar load.  (As a vector load its wait would also be one for the copies under way.)
+template <typename T>
+__device__ __forceinline__ T load_uniform(const T *p) {
+  static_assert(sizeof(T) % 8 == 0, "whole 8 bytes");
+  struct Words {
+    uint64_t w[sizeof(T) / 8];
+  } x;
+  const auto *c = (const __attribute__((address_space(4))) uint64_t *)(uintptr_t)p;
+  static_for<sizeof(T) / 8>([&](auto i) { x.w[int(i)] = c[int(i)]; });
+  return __builtin_bit_cast(T, x);
+}
+
 struct WinPrep {
   const int64_t *cu;
   int64_t n;
@@ -32,33 +45,45 @@ constexpr int kWinMinSteps = 4;   // a part of a split item walks at least 4 key
 // items; it clears the header itself and can split items.
 constexpr int64_t kWinAlonePairs = 131072;
 
+struct WinTile {   // of a tile, what its items need
+  int64_t q_begin, q_end, q_row;
+  int32_t head_begin, head_end;
+};
 struct WinPrepLds {
-  int64_t pre[kPrepThreads];   // units before each tile of the batch
+  WinTile tiles[kPrepThreads];   // a batch of tiles, those outside the buffers without rows
+  int64_t pre[kPrepThreads];     // units before each of them
   int32_t cu[kCuLds];
   int32_t wsum[3][kPrepThreads / 64];
-  long long wunits[kPrepThreads / 64];
-  unsigned long long est, items, work, parts;
-  int32_t base, nslot, nsplit, bad;
+  int64_t wunits[kPrepThreads / 64];
+  unsigned long long est, items, work;
+  int32_t base, at, nslot, nsplit, bad;
 };
+
+__device__ __forceinline__ long long wave_sum(long long v) {
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
 
 // Sums of v over the threads before this one; `total`: over all.  Two barriers.
 __device__ __forceinline__ int block_scan(int v, int32_t *wsum, int &total) {
-  const int tid = threadIdx.x;
+  constexpr int W = kPrepThreads / 64;
+  const int tid = threadIdx.x, l = tid & 63;
   int inc = v;
   for (int o = 1; o < 64; o <<= 1) {
     const int x = __shfl_up(inc, o);
-    if ((tid & 63) >= o) inc += x;
+    if (l >= o) inc += x;
   }
-  if ((tid & 63) == 63) wsum[tid >> 6] = inc;
+  if (l == 63) wsum[tid >> 6] = inc;
   __syncthreads();
-  int before = 0, sum = 0;
-  for (int i = 0; i < kPrepThreads / 64; ++i) {
-    if (i < (tid >> 6)) before += wsum[i];
-    sum += wsum[i];
+  int sum = wsum[l & (W - 1)];   // every wave adds up the waves' sums
+  for (int o = 1; o < W; o <<= 1) {
+    const int x = __shfl_up(sum, o);
+    if ((l & (W - 1)) >= o) sum += x;
   }
-  total = sum;
+  total = __shfl(sum, W - 1);
+  const int before = __shfl(sum, max((tid >> 6) - 1, 0));
   __syncthreads();
-  return before + inc - v;
+  return (tid >= 64 ? before : 0) + inc - v;
 }
 
 // Head chunks (up to 4 query heads of one KV group) of heads [hb, he).
@@ -84,32 +109,136 @@ __device__ __forceinline__ void head_chunk(int hb, int he, int G, int c, int &g,
   nh = min(4, end - h0);
 }
 
-// The items of one head chunk whose first row lies in rows [wa, wb) of a tile
-// (at most 32 rows): f(item), with its steps in kb1 and, in the place of the sample's index,
-// its first key.
+// The item of one head chunk that starts rb rows into the fragment of tile rows [pb, pe) of
+// the sample with first key c0: its steps in kb1 and, in the place of the sample's index, c0.
+__device__ __forceinline__ FwdItem win_item(const WinTile &t, int64_t c0, int64_t pb, int64_t pe,
+                                            int64_t rb, int rows_per, int g, int h0, int nh,
+                                            const Window &win) {
+  const int nrows = (int)(pe - pb - rb < rows_per ? pe - pb - rb : rows_per);
+  const int32_t qmin = (int32_t)(pb + rb - c0), qmax = qmin + nrows - 1;
+  const int w0 = max(0, qmin - win.size + 1) / kFwdBN;   // first block of the window
+  const int far = min((win.sinks + kFwdBN - 1) / kFwdBN, w0);
+  return FwdItem{(int32_t)(t.q_row + (pb + rb - t.q_begin)), qmin, (int32_t)c0, h0, nh, nrows, g,
+                 0, far + qmax / kFwdBN + 1 - w0, -1, far, w0 - far};
+}
+// log2 of the rows of an item of nh heads: 32 (4 / nh).
+__device__ __forceinline__ int item_rows_log2(int nh) { return nh == 1 ? 7 : nh == 2 ? 6 : 5; }
+
+// The items of one head chunk whose first row lies in rows [wa, wb) of a tile (at most 32
+// rows, so at most one of a sample): f(item).
 template <typename F>
-__device__ __forceinline__ void for_each_win_item(const libra_tile_t &t, int64_t wa, int64_t wb,
-                                                  const CuView &cu, int64_t n, int g, int h0,
-                                                  int nh, const Window &win, F &&f) {
-  const int rows_per = kRows * (4 / nh);
+__device__ __forceinline__ void for_each_win_item(const WinTile &t, int64_t wa,
+                                                  int64_t wb, const CuView &cu, int64_t n, int g,
+                                                  int h0, int nh, const Window &win, F &&f) {
+  const int sh = item_rows_log2(nh);
   int64_t j = upper_bound64(cu, n, wa) - 1;
   for (; j < n && cu[j] < wb; ++j) {
     const int64_t c0 = cu[j], c1 = cu[j + 1];
     const int64_t pb = t.q_begin > c0 ? t.q_begin : c0;
     const int64_t pe = t.q_end < c1 ? t.q_end : c1;
-    const int64_t lim = wb < pe ? wb : pe;
-    int64_t k = wa > pb ? (wa - pb + rows_per - 1) / rows_per : 0;
-    for (; pb + k * rows_per < lim; ++k) {
-      const int64_t rb = k * rows_per;
-      const int nrows = (int)(pe - pb - rb < rows_per ? pe - pb - rb : rows_per);
-      const int32_t qmin = (int32_t)(pb + rb - c0), qmax = qmin + nrows - 1;
-      const int w0 = max(0, qmin - win.size + 1) / kFwdBN;   // first block of the window
-      const int far = min((win.sinks + kFwdBN - 1) / kFwdBN, w0);
-      f(FwdItem{(int32_t)(t.q_row + (pb + rb - t.q_begin)), qmin, (int32_t)c0, h0, nh, nrows, g, 0,
-                far + qmax / kFwdBN + 1 - w0, -1, far, w0 - far});
-    }
+    const int64_t rb = wa > pb ? (wa - pb + (1 << sh) - 1) >> sh << sh : 0;
+    if (pb + rb < (wb < pe ? wb : pe)) f(win_item(t, c0, pb, pe, rb, 1 << sh, g, h0, nh, win));
   }
 }
+
+// ---------------------------------------------------------------------------
+// Calls of single tokens (no more Q rows than tiles): no list.  Unit (tile, head chunk, part)
+// finds its work itself, which saves the preparation's launch and most of its time (64
+// sequences, 32 / 8 heads: 20 of 239 us; one: 11 of 25).  A tile of one row has one item of
+// each chunk, cut into up to `parts` key ranges of equal length; of a tile with more rows (the
+// rule allows them) unit p takes every parts-th 32-row window, and its items stay whole.
+struct WinRows {
+  const int64_t *cu;
+  int64_t n;
+  const libra_tile_t *tiles;
+  int64_t T;
+  int h_q, h_kv;
+  int64_t n_q, n_kv;
+  Window win;
+  int32_t *hdr;
+  int chunks;   // head chunks of all heads
+  int parts;    // units of a tile and chunk
+  int64_t units() const { return T * chunks * parts; }
+};
+// Parts of an item of this many steps.
+__device__ __forceinline__ int row_parts(int steps, int parts) {
+  return max(1, min(parts, steps / kWinMinSteps));
+}
+// Last sample that begins at or before x (uniform in the wave): guess, then 64-ary search.
+__device__ __forceinline__ int64_t sample_at(const int64_t *cu, int64_t n, int64_t x,
+                                             int64_t guess) {
+  if (guess < n && load_uniform(cu + guess) <= x && x < load_uniform(cu + guess + 1))
+    return guess;
+  const int lane = threadIdx.x & 63;
+  int64_t lo = 0, count = n;   // the answer is among [lo, lo + count)
+  while (count > 1) {
+    const int64_t step = (count + 63) / 64;
+    const int64_t at = lo + lane * step;
+    const bool le = lane * step < count && cu[at] <= x;
+    const int last = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(le) | 1ull);
+    lo += last * step;
+    count = count - last * step < step ? count - last * step : step;
+  }
+  return lo;
+}
+// Walks the items of one unit; all values are uniform in the workgroup.
+struct RowUnit {
+  WinTile t;
+  int g, h0, nh, p;
+  int64_t job;      // (tile, chunk), numbered
+  int64_t guess;
+  int64_t w, j;     // next window; next sample in it (-1: not looked up)
+  bool valid;
+
+  __device__ __forceinline__ RowUnit(const WinRows &a, int64_t unit) {
+    job = unit / a.parts;
+    p = (int)(unit - job * a.parts);
+    guess = job / a.chunks;
+    const int c = (int)(job - guess * a.chunks);
+    const libra_tile_t tl = load_uniform(a.tiles + guess);
+    t = WinTile{tl.q_begin, tl.q_end, tl.q_row, tl.head_begin, tl.head_end};
+    valid = tile_ok(tl, a.n_q, a.n_kv, a.h_q);
+    if (!valid) return;
+    const int G = a.h_q / a.h_kv;
+    valid = c < head_chunks(t.head_begin, t.head_end, G);
+    if (!valid) return;
+    head_chunk(t.head_begin, t.head_end, G, c, g, h0, nh);
+    w = one_row() ? 0 : p;
+    j = -1;
+  }
+  __device__ __forceinline__ bool one_row() const { return t.q_end - t.q_begin == 1; }
+  // The next item, or false.
+  __device__ __forceinline__ bool next(const WinRows &a, FwdItem &it) {
+    if (!valid) return false;
+    const int sh = item_rows_log2(nh);
+    for (;; w += a.parts, j = -1) {
+      const int64_t wa = t.q_begin + kRows * w;
+      if (wa >= t.q_end) return false;
+      const int64_t wb = wa + kRows < t.q_end ? wa + kRows : t.q_end;
+      if (j < 0) j = sample_at(a.cu, a.n, wa, guess);
+      while (j < a.n) {
+        const int64_t c0 = load_uniform(a.cu + j), c1 = load_uniform(a.cu + j + 1);
+        if (c0 >= wb) break;
+        ++j;
+        const int64_t pb = t.q_begin > c0 ? t.q_begin : c0;
+        const int64_t pe = t.q_end < c1 ? t.q_end : c1;
+        const int64_t rb = wa > pb ? (wa - pb + (1 << sh) - 1) >> sh << sh : 0;
+        if (pb + rb >= (wb < pe ? wb : pe)) continue;
+        it = win_item(t, c0, pb, pe, rb, 1 << sh, g, h0, nh, a.win);
+        if (!one_row()) return true;
+        const int np = row_parts(it.kb1, a.parts), per = (it.kb1 + np - 1) / np;
+        valid = false;   // the only one
+        if (p * per >= it.kb1) return false;
+        if (np > 1) {
+          it.kb0 = p * per;
+          it.kb1 = min((p + 1) * per, it.kb1);
+          it.slot = (int32_t)(job * a.parts + p);
+        }
+        return true;
+      }
+    }
+  }
+};
 
 // Clears the header of a windowed call (one workgroup of kPrepThreads): the lists are
 // empty, hold up to max_q and max_kv items and are run by grid_q and grid_kv workgroups.
@@ -139,85 +268,100 @@ __device__ __forceinline__ void clear_win_header(int32_t *hdr, int grid_q, int64
 // its order, so that nothing depends on which part runs where.
 __device__ __forceinline__ void prep_win(const WinPrep &a, WinPrepLds &lds, unsigned block,
                                          unsigned blocks) {
-  const int tid = threadIdx.x, G = a.h_q / a.h_kv;
+  const int tid = threadIdx.x, l = tid & 63, G = a.h_q / a.h_kv;
   const int64_t n = a.n, T = a.T;
   const CuView cu = cu_view(a.cu, n, lds.cu);
   if (tid == 0) {
-    lds.est = lds.items = lds.work = lds.parts = 0;
+    lds.est = lds.items = lds.work = 0;
     lds.base = lds.nslot = lds.nsplit = lds.bad = 0;
   }
   __syncthreads();
-  // items at least, and the tiles outside the buffers
-  {
-    unsigned long long est = 0;
-    int bad = 0;
-    for (int64_t t = tid; t < T; t += kPrepThreads) {
-      const libra_tile_t tl = a.tiles[t];
-      if (!tile_ok(tl, a.n_q, a.n_kv, a.h_q)) {
-        ++bad;
-        continue;
+  // The tiles [tb, tb + kPrepThreads) and the units before each; returns the units of all.
+  // `first`: also counts the items at least, and the tiles outside the buffers.
+  auto load = [&](int64_t tb, bool first) {
+    WinTile wt{};
+    int64_t u = 0;
+    long long est = 0;
+    bool bad = false;
+    if (tb + tid < T) {
+      const libra_tile_t tl = a.tiles[tb + tid];
+      bad = !tile_ok(tl, a.n_q, a.n_kv, a.h_q);
+      if (!bad) {
+        wt = WinTile{tl.q_begin, tl.q_end, tl.q_row, tl.head_begin, tl.head_end};
+        const int chunks = head_chunks(tl.head_begin, tl.head_end, G);
+        u = (tl.q_end - tl.q_begin + kRows - 1) / kRows * chunks;
+        est = (tl.q_end - tl.q_begin + 127) / 128 * chunks;
       }
-      est += (unsigned long long)((tl.q_end - tl.q_begin + 127) / 128) *
-             (unsigned)head_chunks(tl.head_begin, tl.head_end, G);
     }
-    if (est) atomicAdd(&lds.est, est);
-    if (bad) atomicAdd(&lds.bad, bad);
+    if (first) {
+      est = wave_sum(est);
+      const int b = __builtin_popcountll(__builtin_amdgcn_ballot_w64(bad));
+      if (l == 0 && est) atomicAdd(&lds.est, (unsigned long long)est);
+      if (l == 0 && b) atomicAdd(&lds.bad, b);
+    }
+    lds.tiles[tid] = wt;
+    long long inc = u;
+    for (int o = 1; o < 64; o <<= 1) {
+      const long long x = __shfl_up(inc, o);
+      if (l >= o) inc += x;
+    }
+    if (l == 63) lds.wunits[tid >> 6] = inc;
     __syncthreads();
-  }
+    constexpr int W = kPrepThreads / 64;
+    long long sum = lds.wunits[l & (W - 1)];
+    for (int o = 1; o < W; o <<= 1) {
+      const long long x = __shfl_up(sum, o);
+      if ((l & (W - 1)) >= o) sum += x;
+    }
+    const int64_t total = __shfl(sum, W - 1);
+    const long long before = __shfl(sum, max((tid >> 6) - 1, 0));
+    lds.pre[tid] = (tid >= 64 ? before : 0) + inc - u;
+    __syncthreads();
+    return total;
+  };
+  int64_t total = 0;
+  for (int64_t tb = 0; tb < T; tb += kPrepThreads) total = load(tb, true);
+  // the header's clearing stores, if this workgroup made them, come before what follows
+  wait_vm_known();
+  __syncthreads();
+  const bool one_batch = T <= kPrepThreads;   // then it stays loaded
   const bool few = lds.est < 2ull * (unsigned)a.split_grid;
   const bool alone = blocks == 1 || few;
   if (alone && block) return;
   if (tid == 0 && block == 0 && a.count_bad && lds.bad) atomicAdd(&a.hdr[kBadTiles], lds.bad);
   const unsigned nb = alone ? 1 : blocks;
 
-  // every unit of this workgroup: f(tile, first row, end, KV head, first head, heads), by
-  // rounds of one unit to a thread (valid says whether it has one), for all threads alike
+  // every unit of this workgroup: f(valid, tile, first row, end, KV head, first head, heads),
+  // by rounds of one unit to a thread (valid: it has one), for all threads alike
   auto units = [&](auto &&f) {
     for (int64_t tb = 0; tb < T; tb += kPrepThreads) {
-      long long u = 0;
-      if (tb + tid < T) {
-        const libra_tile_t tl = a.tiles[tb + tid];
-        if (tile_ok(tl, a.n_q, a.n_kv, a.h_q))
-          u = (tl.q_end - tl.q_begin + kRows - 1) / kRows *
-              head_chunks(tl.head_begin, tl.head_end, G);
+      if (!one_batch) {
+        __syncthreads();   // the batch before is done with
+        total = load(tb, false);
       }
-      long long inc = u;
-      for (int o = 1; o < 64; o <<= 1) {
-        const long long x = __shfl_up(inc, o);
-        if ((tid & 63) >= o) inc += x;
-      }
-      __syncthreads();   // the batch before is done with `pre`
-      if ((tid & 63) == 63) lds.wunits[tid >> 6] = inc;
-      __syncthreads();
-      long long before = 0, total = 0;
-      for (int i = 0; i < kPrepThreads / 64; ++i) {
-        if (i < (tid >> 6)) before += lds.wunits[i];
-        total += lds.wunits[i];
-      }
-      lds.pre[tid] = before + inc - u;
-      __syncthreads();
-      const long long ua = total / nb * block + total % nb * block / nb;
-      const long long ub = total / nb * (block + 1) + total % nb * (block + 1) / nb;
-      for (long long v0 = ua; v0 < ub; v0 += kPrepThreads) {
-        const long long v = v0 + tid;
+      const int64_t ua = total / nb * block + total % nb * block / nb;
+      const int64_t ub = total / nb * (block + 1) + total % nb * (block + 1) / nb;
+      for (int64_t v0 = ua; v0 < ub; v0 += kPrepThreads) {
+        const int64_t v = v0 + tid;
         const bool valid = v < ub;
-        libra_tile_t tl{};
+        WinTile tl{};
         int64_t wa = 0, wb = 0;
         int g = 0, h0 = 0, nh = 1;
         if (valid) {
           // the last tile with no more units before it
-          int lo = 0, hi = kPrepThreads;
+          int lo = 0, hi = (int)(T - tb < kPrepThreads ? T - tb : kPrepThreads);
           while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (lds.pre[mid] <= v) lo = mid; else hi = mid;
           }
-          tl = a.tiles[tb + lo];
+          tl = lds.tiles[lo];
           const int64_t windows = (tl.q_end - tl.q_begin + kRows - 1) / kRows;
-          const long long r = v - lds.pre[lo];
-          const int c = (int)(r / windows);
+          const int64_t r = v - lds.pre[lo];
+          const int64_t c = (r | windows) >> 32 ? r / windows
+                                                : (int64_t)((uint32_t)r / (uint32_t)windows);
           wa = tl.q_begin + kRows * (r - c * windows);
           wb = wa + kRows < tl.q_end ? wa + kRows : tl.q_end;
-          head_chunk(tl.head_begin, tl.head_end, G, c, g, h0, nh);
+          head_chunk(tl.head_begin, tl.head_end, G, (int)c, g, h0, nh);
         }
         f(valid, tl, wa, wb, g, h0, nh);
       }
@@ -226,16 +370,18 @@ __device__ __forceinline__ void prep_win(const WinPrep &a, WinPrepLds &lds, unsi
 
   int chunk = 0;   // steps of a part; 0: no item is split
   if (alone && few && a.max_parts > 0) {
-    units([&](bool valid, const libra_tile_t &tl, int64_t wa, int64_t wb, int g, int h0, int nh) {
-      if (!valid) return;
-      unsigned long long items = 0, work = 0;
-      for_each_win_item(tl, wa, wb, cu, n, g, h0, nh, a.win, [&](const FwdItem &it) {
-        ++items;
-        work += (unsigned)it.kb1;
-      });
-      if (items) {
-        atomicAdd(&lds.items, items);
-        atomicAdd(&lds.work, work);
+    units([&](bool valid, const WinTile &tl, int64_t wa, int64_t wb, int g, int h0, int nh) {
+      long long items = 0, work = 0;
+      if (valid)
+        for_each_win_item(tl, wa, wb, cu, n, g, h0, nh, a.win, [&](const FwdItem &it) {
+          ++items;
+          work += it.kb1;
+        });
+      items = wave_sum(items);
+      work = wave_sum(work);
+      if (l == 0 && items) {
+        atomicAdd(&lds.items, (unsigned long long)items);
+        atomicAdd(&lds.work, (unsigned long long)work);
       }
     });
     __syncthreads();
@@ -253,7 +399,7 @@ __device__ __forceinline__ void prep_win(const WinPrep &a, WinPrepLds &lds, unsi
   auto parts_of = [&](const FwdItem &it) {
     return chunk && it.kb1 >= 2 * chunk ? (it.kb1 + chunk - 1) / chunk : 1;
   };
-  units([&](bool valid, const libra_tile_t &tl, int64_t wa, int64_t wb, int g, int h0, int nh) {
+  units([&](bool valid, const WinTile &tl, int64_t wa, int64_t wb, int g, int h0, int nh) {
     int items = 0, slots = 0, cut = 0;
     if (valid)
       for_each_win_item(tl, wa, wb, cu, n, g, h0, nh, a.win, [&](const FwdItem &it) {
@@ -268,23 +414,19 @@ __device__ __forceinline__ void prep_win(const WinPrep &a, WinPrepLds &lds, unsi
     if (chunk) {
       slot = lds.nslot + block_scan(slots, lds.wsum[1], all_slots);
       sp = lds.nsplit + block_scan(cut, lds.wsum[2], all_cut);
+      __syncthreads();
     }
-    __syncthreads();
     if (tid == 0) {
-      if (alone) {
-        lds.parts = (unsigned long long)lds.base;
-        lds.base += all;
-      } else {
-        lds.parts = (unsigned)atomicAdd(&a.hdr[kFwdQ + kXcds], all);
-      }
+      lds.at = alone ? lds.base : atomicAdd(&a.hdr[kFwdQ + kXcds], all);
+      lds.base += all;
       // the run that reaches past the list (overlapping tiles can fill it)
-      if ((long long)lds.parts <= a.max_items && (long long)lds.parts + all > a.max_items)
+      if (lds.at <= a.max_items && (int64_t)lds.at + all > a.max_items)
         atomicAdd(&a.hdr[a.count_bad ? kBadTiles : kDqFull], 1);
       lds.nslot += all_slots;
       lds.nsplit += all_cut;
     }
     __syncthreads();
-    int64_t at = before_items + (int64_t)lds.parts;
+    int64_t at = (int64_t)lds.at + before_items;
     if (valid)
       for_each_win_item(tl, wa, wb, cu, n, g, h0, nh, a.win, [&](const FwdItem &it) {
         const int np = parts_of(it), per = (it.kb1 + np - 1) / np;
@@ -335,7 +477,8 @@ struct WinSink {
   int32_t base, parts;
 };
 constexpr int kMaxSinks = 1024;
-constexpr int kSinkParts = 1024;   // slots beyond one for each WinSink
+constexpr int kSinkPartRows = 128;   // rows of a part of far rows at least
+constexpr int kSinkParts = 512;    // slots beyond one for each WinSink
 __host__ __device__ constexpr int sink_blocks(const Window &w) { return (w.sinks + 31) / 32; }
 __host__ __device__ constexpr size_t sink_part_floats(int d) { return (size_t)2 * 32 * d; }
 // First 128-key block in the window of the row at sample-local position p.
@@ -366,13 +509,17 @@ struct WinBwdPrep {
   BwdItem *sink_items;  // (sample, 32 sinks, KV head) x far rows
 };
 
-// Can a call split an item?  One of two parts or more: its rows' window, the rows (at
-// most 128) and the sinks have to reach over that many blocks.
-inline bool win_may_split(const Window &w, int64_t n_kv) {
+// Steps of an item at most: its rows' window, the rows (at most 128) and the sinks.
+inline int64_t win_max_steps(const Window &w, int64_t n_kv) {
   const int64_t reach = (int64_t)w.size + kFwdPartRows + kFwdBN;
-  return (reach < n_kv ? reach : n_kv) / kFwdBN + 1 + (w.sinks + kFwdBN - 1) / kFwdBN >=
-         2 * kWinMinSteps;
+  return (reach < n_kv ? reach : n_kv) / kFwdBN + 1 + (w.sinks + kFwdBN - 1) / kFwdBN;
 }
+// Can a call split an item?  One of two parts or more.
+inline bool win_may_split(const Window &w, int64_t n_kv) {
+  return win_max_steps(w, n_kv) >= 2 * kWinMinSteps;
+}
+// Single tokens beyond this many (tile, head chunk) pairs go through the list.
+constexpr int64_t kMaxRowJobs = 1 << 20;
 
 // Arguments of the windowed dQ kernel (attn_window_dq.hip).  q and o, or q8 and o8.
 struct WinDq {

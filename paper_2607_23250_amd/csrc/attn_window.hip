@@ -25,8 +25,6 @@ namespace libra {
 __global__ __launch_bounds__(kPrepThreads) void win_alone_kernel(WinPrep a) {
   __shared__ WinPrepLds lds;
   clear_win_header(a.hdr, a.grid, a.max_items, 0, 0);
-  __threadfence();
-  __syncthreads();
   prep_win(a, lds, 0, 1);
 }
 __global__ __launch_bounds__(kPrepThreads) void win_clear_kernel(int32_t *hdr, int grid,
@@ -131,8 +129,8 @@ __global__ __launch_bounds__(kPrepThreads) void win_tiles_kernel(WinPrep q, WinB
   else win_tile(b, blockIdx.x - item_blocks);
 }
 
-// Workgroup 0: the WinSink records and the items of the far rows: parts of C rows, so that
-// there are at most kSinkParts more of them than records.
+// Workgroup 0: the WinSink records and the items of the far rows: parts of equal row ranges,
+// so that there are at most kSinkParts (two for each CU) more of them than records.
 __device__ __forceinline__ void win_far_items(const WinBwdPrep &a, int32_t *wsum,
                                               unsigned long long *total_rows) {
   const int tid = threadIdx.x, nsb = sink_blocks(a.win), per = a.h_kv * nsb;
@@ -157,7 +155,7 @@ __device__ __forceinline__ void win_far_items(const WinBwdPrep &a, int32_t *wsum
   __syncthreads();
   const unsigned long long total = *total_rows;
   const long long c = (long long)((total + kSinkParts - 1) / kSinkParts);
-  const long long chunk = c > kFarRows ? (c + kRows - 1) / kRows * kRows : kFarRows;
+  const long long chunk = c > kSinkPartRows ? (c + kRows - 1) / kRows * kRows : kSinkPartRows;
   int count = 0;
   for (int e0 = 0; e0 < nfar * per; e0 += kPrepThreads) {
     const int e = e0 + tid;
@@ -304,7 +302,7 @@ win_sink_kernel(const f16 *__restrict__ k, const f16 *__restrict__ v,
       dva[dt] = mfma_zero_c();
       dka[dt] = mfma_zero_c();
     });
-    StepIter it{a.tiles, (int64_t)item.t1 + 1, a.n_q, a.n_kv, key0, key0 + item.r0,
+    StepIter<true> it{a.tiles, (int64_t)item.t1 + 1, a.n_q, a.n_kv, key0, key0 + item.r0,
                 key0 + item.r1, a.h_q, item.g, G, 0, 2 * S::HEAD_EL / 1024};
     it.start(item.t0);
     // this wave's units: the heads of every fourth step, the copy of the next one under way

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(kThreads, 2) void win_dq_kernel(WinDq a) {
   for (;; turn ^= 1) {
     const int idx = __builtin_amdgcn_readfirstlane(s_next[turn]);
     if (idx < 0) break;
-    const FwdItem it = a.items[idx];
+    const FwdItem it = load_uniform(a.items + idx);
     const int key0 = it.sample;   // its first key
     const int head = it.head0 + (w % it.nh);
     const int wrow0 = (w / it.nh) * kRows;
