@@ -489,20 +489,20 @@ constexpr int kTileSplit = 64;
 // WIN: nor does any write the other parts of those rows (the dQ kernel writes the records
 // there).  HELD: q in 8 bits.
 template <int D, bool WIN, bool HELD>
-__device__ __forceinline__ void absmax_q(unsigned block, const bf16 *__restrict__ q,
-                                         const Held &q8,
+__device__ __forceinline__ void absmax_q(unsigned block, unsigned split,
+                                         const bf16 *__restrict__ q, const Held &q8,
                                          const bf16 *__restrict__ dout,
                                          const libra_tile_t *__restrict__ tiles, int h_q,
                                          int64_t n_q, int64_t n_kv, int64_t pool,
                                          int32_t *__restrict__ hdr, f16 *__restrict__ rec) {
   const int tid = threadIdx.x;
-  const libra_tile_t tl = tiles[block / kTileSplit];
+  const libra_tile_t tl = tiles[block / split];
   if (!tile_ok(tl, n_q, n_kv, h_q)) return;
   const int64_t ra = tl.q_row, rb = tl.q_row + (tl.q_end - tl.q_begin);
   const int r = tid >> 3, part = tid & 7;   // 8 threads per row, 32 rows per pass
   const int64_t past = tl.q_row + (pool - tl.q_begin);   // first row past the last sample
   float mq = 0.f, mo = 0.f;
-  for (int64_t m = ra / kRows + block % kTileSplit; m * kRows < rb; m += kTileSplit) {
+  for (int64_t m = ra / kRows + block % split; m * kRows < rb; m += split) {
     const int64_t row = m * kRows + r;
     const bool ok = row >= ra && row < rb && !(WIN && row >= past);
     if constexpr (WIN) {
@@ -717,6 +717,7 @@ struct BwdPass {
   unsigned tile_blocks, kv_blocks, zero_blocks;
   Window win;
   Held q8;
+  unsigned tile_split;   // windowed: workgroups of a tile in the max pass
 };
 template <int D, bool WIN, bool HELD>
 __global__ __launch_bounds__(256) void bwd_max_kernel(BwdPass a) {
@@ -726,7 +727,7 @@ __global__ __launch_bounds__(256) void bwd_max_kernel(BwdPass a) {
     kv_pass<D, false, WIN>(b, a.kv_blocks, a.k, a.v, a.cu, a.n, a.ext, a.h_kv, a.n_kv, a.hdr,
                            a.k16, a.v16, a.win);
   } else if ((b -= a.kv_blocks) < a.tile_blocks) {
-    absmax_q<D, WIN, HELD>(b, a.q, a.q8, a.dout, a.tiles, a.h_q, a.n_q, a.n_kv, a.cu[a.n], a.hdr, a.rec);
+    absmax_q<D, WIN, HELD>(b, WIN ? a.tile_split : kTileSplit, a.q, a.q8, a.dout, a.tiles, a.h_q, a.n_q, a.n_kv, a.cu[a.n], a.hdr, a.rec);
   } else {
     b -= a.tile_blocks;
     const unsigned half = a.zero_blocks / 2;
@@ -1148,7 +1149,7 @@ __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 
     if constexpr (WIN) {
       // the far rows of this wave's sinks (places as written by win_sink_sum_kernel)
       const int first = samples[item.sample].far;   // -1: no far row is covered
-      if (first >= 0 && kw0 < win.sinks) {
+      if (first >= 0 && kw0 < win.sinks && item.r0 == 0) {   // in a split item's first part
         const WinSink sk = sinks[first + g * sink_blocks(win) + kw0 / 32];
         if (sk.parts > 0) {
           const float *src = sink_parts + (size_t)sk.base * sink_part_floats(D) +
@@ -1216,11 +1217,13 @@ __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 
 // Sums the parts of every split dK / dV item (hdr[kBwdSplits] records) in row
 // order and writes dK and dV as the kernel does for whole items.  Work shared
 // as in fwd_combine_kernel (16 keys to a workgroup, 16 threads to a key).
-template <int D>
+// WIN: keys past a sample's last covered row have no sums.
+template <int D, bool WIN>
 __global__ __launch_bounds__(256) void bwd_dkdv_combine_kernel(
     const BwdSplit *__restrict__ splits, const int32_t *__restrict__ hdr,
     const float *__restrict__ parts, const int64_t *__restrict__ cu, int h_kv, float scale,
-    void *__restrict__ dk_out, void *__restrict__ dv_out, int accumulate) {
+    void *__restrict__ dk_out, void *__restrict__ dv_out, int accumulate,
+    const WinSample *__restrict__ samples) {
   constexpr size_t PF = fwd_part_floats(D);
   constexpr int W = D / kCombineThreads;   // columns of a thread
   const int count = hdr[kBwdSplits] * kCombineSplit;
@@ -1233,7 +1236,7 @@ __global__ __launch_bounds__(256) void bwd_dkdv_combine_kernel(
     const BwdSplit sp = splits[e / kCombineSplit];
     const int kr = e % kCombineSplit * kCombineRows + tid / kCombineThreads;
     const int64_t key0 = cu[sp.item.sample], key = key0 + (int64_t)sp.item.kb * kBwdBK + kr;
-    if (key >= cu[sp.item.sample + 1]) continue;
+    if (key >= (WIN ? key0 + samples[sp.item.sample].ext : cu[sp.item.sample + 1])) continue;
     const float *src = parts + (size_t)sp.base * 2 * PF + (size_t)kr * D + col;
     float acc[2][W];
 #pragma unroll
@@ -1286,7 +1289,7 @@ BwdLayout bwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, i
   const int64_t key_blocks = n_kv / kBwdBK + n + 1;
   // a split item's parts take its place: kBwdSplitSlots of them at most
   L.max_blocks = key_blocks * (int64_t)h_kv;
-  L.max_items = L.max_blocks + (w ? 0 : kBwdSplitSlots);
+  L.max_items = L.max_blocks + kBwdSplitSlots;
   L.max_qitems = fwd_max_items(T, n, n_q, h_q, h_kv);
   L.nq_pad = (n_q + kRows - 1) / kRows * kRows;
   L.hdr = 0;
@@ -1311,7 +1314,8 @@ BwdLayout bwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, i
     L.far_list = align256b(L.bsplits + (size_t)sinks * sizeof(WinSink));
     L.sink_items = align256b(L.far_list + (size_t)far * sizeof(int32_t));
     L.sink_parts = align256b(L.sink_items + (size_t)slots * sizeof(BwdItem));
-    L.parts = align256b(L.sink_parts + (size_t)slots * sink_part_floats(d) * sizeof(float));
+    L.kv_splits = align256b(L.sink_parts + (size_t)slots * sink_part_floats(d) * sizeof(float));
+    L.parts = align256b(L.kv_splits + (size_t)kWinMaxSplits * sizeof(BwdSplit));
     L.far = far;
   } else {
     L.cov = align256b(L.bsplits + (size_t)(kBwdSplitSlots / 2) * sizeof(BwdSplit));
@@ -1377,7 +1381,9 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
                       reinterpret_cast<WinBlock *>(ws + L.gmask), L.max_blocks / h_kv, items,
                       L.max_items, reinterpret_cast<WinSink *>(ws + L.bsplits),
                       reinterpret_cast<int32_t *>(ws + L.far_list),
-                      reinterpret_cast<BwdItem *>(ws + L.sink_items)};
+                      reinterpret_cast<BwdItem *>(ws + L.sink_items), cus,
+                      reinterpret_cast<BwdSplit *>(ws + L.kv_splits),
+                      win_kv_parts(win, L.max_blocks / h_kv, h_kv, cus)};
       launch_win_prep_bwd(WinPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, win, hdr, qitems,
                                   L.max_qitems, 0, cus * kWinDqPerCu, cus * kWinDqPerCu,
                                   max_parts, 0, splits}, wb, cus, st);
@@ -1395,10 +1401,17 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
     // 4096 rows)
     const unsigned kv_blocks =
         (unsigned)std::max<int64_t>(1, std::min<int64_t>((n_kv + 31) / 32, (int64_t)cus * 8));
-    const BwdPass pass{q, k, v, o, dout, lse, cu, n, tiles, h_q, h_kv, n_q, n_kv, L.nq_pad, scale,
+    BwdPass pass{q, k, v, o, dout, lse, cu, n, tiles, h_q, h_kv, n_q, n_kv, L.nq_pad, scale,
                        hdr, ext, rec, k16, v16, stats, static_cast<uint4 *>(dk),
                        static_cast<uint4 *>(dv), n16, (unsigned)(T * kTileSplit), kv_blocks,
-                       2 * zero_blocks, win, q8};
+                       2 * zero_blocks, win, q8, 1};
+    if constexpr (WIN) {
+      // Eight workgroups per CU in all: each looks at the maxima found so far, one address
+      // for all of them (68 tiles of a 20K pack: 44 us with 64 for each tile, 31 with 15; the
+      // 32 tiles of a 32K pack: 155 us with 64, 171 with 32).
+      pass.tile_split = (unsigned)std::max<int64_t>(1, std::min<int64_t>(kTileSplit, 8 * cus / T));
+      pass.tile_blocks = (unsigned)T * pass.tile_split;
+    }
     hipLaunchKernelGGL(HIP_KERNEL_NAME(bwd_max_kernel<D, WIN, HELD>),
                        dim3(pass.kv_blocks + pass.tile_blocks + pass.zero_blocks), dim3(256), 0,
                        st, pass);
@@ -1432,10 +1445,11 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
                        KvShape<D>::SMEM, st, k16, v16, rec, cu, tiles, T, items, hdr, h_q, h_kv,
                        n_q, n_kv, scale, scale * kLog2e, dk, dv, accumulate ? 1 : 0, parts, win,
                        samples, wb.sinks, sink_parts);
-    if (!WIN && may_split_rows(n_kv))
-      hipLaunchKernelGGL(bwd_dkdv_combine_kernel<D>, dim3(cus * 4), dim3(256), 0, st,
-                         reinterpret_cast<const BwdSplit *>(ws + L.bsplits), hdr, parts, cu, h_kv,
-                         scale, dk, dv, accumulate ? 1 : 0);
+    if (WIN ? wb.parts > 1 : may_split_rows(n_kv))
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(bwd_dkdv_combine_kernel<D, WIN>), dim3(cus * 4),
+                         dim3(256), 0, st,
+                         WIN ? wb.splits : reinterpret_cast<const BwdSplit *>(ws + L.bsplits), hdr,
+                         parts, cu, h_kv, scale, dk, dv, accumulate ? 1 : 0, samples);
     if (tm_kv) hipEventRecord(tm_kv->end, st);
   }
   const hipError_t e = hipGetLastError();

@@ -736,7 +736,7 @@ struct BwdLayout {
   size_t hdr = 0, ext = 0, gmask = 0, items = 0, qitems = 0, rec = 0, k16 = 0,
          v16 = 0, stats = 0, splits = 0, bsplits = 0, cov = 0, parts = 0, total = 0;
   // windowed: WinSample records at ext, WinBlock at gmask, WinSink at bsplits
-  size_t far_list = 0, sink_items = 0, sink_parts = 0;
+  size_t far_list = 0, sink_items = 0, sink_parts = 0, kv_splits = 0;
   int64_t far = 0;   // far samples at most
   int32_t max_parts = 0;   // split-K partial slots of the dQ kernel
   int64_t max_blocks = 0, max_items = 0, max_qitems = 0, nq_pad = 0;

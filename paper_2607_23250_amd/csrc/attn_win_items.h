@@ -92,6 +92,20 @@ __device__ __forceinline__ int head_chunks(int hb, int he, int G) {
   if (g0 == g1) return (he - hb + 3) / 4;
   return ((g0 + 1) * G - hb + 3) / 4 + (g1 - g0 - 1) * ((G + 3) / 4) + (he - g1 * G + 3) / 4;
 }
+// log2 of the rows of an item of nh heads: 32 (4 / nh).
+__device__ __forceinline__ int item_rows_log2(int nh) { return nh == 1 ? 7 : nh == 2 ? 6 : 5; }
+
+// Items of heads [hb, he) x rows that lie in one sample.
+__device__ __forceinline__ int64_t items_of(int64_t rows, int hb, int he, int G) {
+  auto of = [&](int heads) {
+    const int rest = heads & 3, sh = item_rows_log2(rest);
+    return heads / 4 * ((rows + kRows - 1) / kRows) +
+           (rest ? (rows + (1 << sh) - 1) >> sh : (int64_t)0);
+  };
+  const int g0 = hb / G, g1 = (he - 1) / G;
+  if (g0 == g1) return of(he - hb);
+  return of((g0 + 1) * G - hb) + (g1 - g0 - 1) * of(G) + of(he - g1 * G);
+}
 // Chunk c of them: its KV head, first query head and heads.
 __device__ __forceinline__ void head_chunk(int hb, int he, int G, int c, int &g, int &h0,
                                            int &nh) {
@@ -121,8 +135,6 @@ __device__ __forceinline__ FwdItem win_item(const WinTile &t, int64_t c0, int64_
   return FwdItem{(int32_t)(t.q_row + (pb + rb - t.q_begin)), qmin, (int32_t)c0, h0, nh, nrows, g,
                  0, far + qmax / kFwdBN + 1 - w0, -1, far, w0 - far};
 }
-// log2 of the rows of an item of nh heads: 32 (4 / nh).
-__device__ __forceinline__ int item_rows_log2(int nh) { return nh == 1 ? 7 : nh == 2 ? 6 : 5; }
 
 // The items of one head chunk whose first row lies in rows [wa, wb) of a tile (at most 32
 // rows, so at most one of a sample): f(item).
@@ -290,7 +302,7 @@ __device__ __forceinline__ void prep_win(const WinPrep &a, WinPrepLds &lds, unsi
         wt = WinTile{tl.q_begin, tl.q_end, tl.q_row, tl.head_begin, tl.head_end};
         const int chunks = head_chunks(tl.head_begin, tl.head_end, G);
         u = (tl.q_end - tl.q_begin + kRows - 1) / kRows * chunks;
-        est = (tl.q_end - tl.q_begin + 127) / 128 * chunks;
+        est = items_of(tl.q_end - tl.q_begin, tl.head_begin, tl.head_end, G);
       }
     }
     if (first) {
@@ -478,7 +490,7 @@ struct WinSink {
 };
 constexpr int kMaxSinks = 1024;
 constexpr int kSinkPartRows = 128;   // rows of a part of far rows at least
-constexpr int kSinkParts = 512;    // slots beyond one for each WinSink
+constexpr int kSinkParts = 256;      // slots beyond one for each WinSink
 __host__ __device__ constexpr int sink_blocks(const Window &w) { return (w.sinks + 31) / 32; }
 __host__ __device__ constexpr size_t sink_part_floats(int d) { return (size_t)2 * 32 * d; }
 // First 128-key block in the window of the row at sample-local position p.
@@ -507,7 +519,19 @@ struct WinBwdPrep {
   WinSink *sinks;       // one for each far sample, KV head and 32 sinks
   int32_t *far_list;    // far samples with covered far rows
   BwdItem *sink_items;  // (sample, 32 sinks, KV head) x far rows
+  int cus;
+  BwdSplit *splits;     // dK / dV items cut into `parts` row ranges each (1: none)
+  int parts;
 };
+// Row ranges of a dK / dV item.  A call of few key blocks and KV heads (4K tokens and 2 KV
+// heads: 66 items for 256 CUs) cuts each into as many as the CUs hold, of at least 8 row blocks.
+inline int win_kv_parts(const Window &w, int64_t key_blocks, int h_kv, int cus) {
+  const int64_t fit = cus / (key_blocks * h_kv);
+  const int64_t most = ((int64_t)w.size + kBwdBK) / (kBwdSplitMinBlocks * kRows);
+  const int64_t n = fit < most ? fit : most;
+  return (int)(n < 1 ? 1 : n > 8 ? 8 : n);
+}
+constexpr int kWinMaxSplits = 512;   // split dK / dV items of a call (more than CUs / 2)
 
 // Steps of an item at most: its rows' window, the rows (at most 128) and the sinks.
 inline int64_t win_max_steps(const Window &w, int64_t n_kv) {

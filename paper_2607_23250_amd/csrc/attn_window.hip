@@ -130,7 +130,7 @@ __global__ __launch_bounds__(kPrepThreads) void win_tiles_kernel(WinPrep q, WinB
 }
 
 // Workgroup 0: the WinSink records and the items of the far rows: parts of equal row ranges,
-// so that there are at most kSinkParts (two for each CU) more of them than records.
+// at most kSinkParts more of them than records.
 __device__ __forceinline__ void win_far_items(const WinBwdPrep &a, int32_t *wsum,
                                               unsigned long long *total_rows) {
   const int tid = threadIdx.x, nsb = sink_blocks(a.win), per = a.h_kv * nsb;
@@ -154,7 +154,10 @@ __device__ __forceinline__ void win_far_items(const WinBwdPrep &a, int32_t *wsum
   __threadfence();
   __syncthreads();
   const unsigned long long total = *total_rows;
-  const long long c = (long long)((total + kSinkParts - 1) / kSinkParts);
+  // one item for each CU, counting the odd end that every record can have: with twice as
+  // many, their preparation and merging took a tenth longer (32K pack, 16K sample: [SINKT])
+  const long long want = min(max(a.cus - nfar * per, a.cus / 2), kSinkParts);
+  const long long c = (long long)((total + want - 1) / want);
   const long long chunk = c > kSinkPartRows ? (c + kRows - 1) / kRows * kRows : kSinkPartRows;
   int count = 0;
   for (int e0 = 0; e0 < nfar * per; e0 += kPrepThreads) {
@@ -185,6 +188,8 @@ __device__ __forceinline__ void win_far_items(const WinBwdPrep &a, int32_t *wsum
 }
 
 // The dK / dV items, by KV head, then key block; and (workgroup 0) those of the far rows.
+// Calls that cut them (a.parts > 1) have a single workgroup for it, so that slots and split
+// records are numbered the same from one call to the next.
 __global__ __launch_bounds__(kPrepThreads) void win_kv_items_kernel(WinBwdPrep a) {
   __shared__ int32_t wsum[kPrepThreads / 64];
   __shared__ int32_t base;
@@ -195,13 +200,14 @@ __global__ __launch_bounds__(kPrepThreads) void win_kv_items_kernel(WinBwdPrep a
     return;
   }
   const int64_t places = a.n_blocks * a.h_kv;
+  int splits = 0;
   const unsigned blocks = gridDim.x - 1, block = blockIdx.x - 1;
   const int64_t share = (places + blocks - 1) / blocks;
   const int64_t pa = share * block, pb = pa + share < places ? pa + share : places;
   for (int64_t p0 = pa; p0 < pb; p0 += kPrepThreads) {
     const int64_t p = p0 + tid;
     BwdItem it{};
-    int has = 0;
+    int has = 0, end_row = 0;   // end_row: of the rows that the item can meet
     if (p < pb) {
       const int g = (int)(p / a.n_blocks);
       const int64_t at = p - g * a.n_blocks;
@@ -221,15 +227,35 @@ __global__ __launch_bounds__(kPrepThreads) void win_kv_items_kernel(WinBwdPrep a
         it = BwdItem{(int32_t)lo, kb, g, -1, 0,
                      all || end > INT32_MAX ? INT32_MAX : (int32_t)end, b.t0, b.t1};
         has = 1;
+        end_row = min(it.r1, a.samples[lo].ext);
       }
     }
     int all;
     const int at = block_scan(has, wsum, all);
-    if (tid == 0) base = all ? atomicAdd(&a.hdr[kBwdQ + kXcds], all) : 0;
+    if (tid == 0) base = all ? atomicAdd(&a.hdr[kBwdQ + kXcds], all * a.parts) : 0;
     __syncthreads();
-    if (has && base + at < a.max_items) a.items[base + at] = it;
-    __syncthreads();
+    const int64_t to = base + (int64_t)at * a.parts;
+    if (has && to + a.parts <= a.max_items) {
+      if (a.parts > 1) {
+        // equal ranges of whole 32-row blocks; the slots of an item are numbered by its place
+        const int first = it.kb * kBwdBK, np = a.parts;
+        const int per = max(kRows, ((end_row - first + np - 1) / np + kRows - 1) / kRows * kRows);
+        const int n = (int)(to / np);
+        a.splits[n] = BwdSplit{it, n * np, np, 0, 0};
+        const int r1 = it.r1;
+        for (int q = 0; q < np; ++q) {
+          it.slot = n * np + q;
+          it.r0 = q ? first + q * per : 0;
+          it.r1 = q + 1 < np ? min(first + (q + 1) * per, r1) : r1;
+          a.items[to + q] = it;
+        }
+      } else {
+        a.items[to] = it;
+      }
+    }
+    splits += all;
   }
+  if (a.parts > 1 && tid == 0) a.hdr[kBwdSplits] = splits;
 }
 
 void launch_win_prep_bwd(const WinPrep &q, const WinBwdPrep &b, int grid_kv, hipStream_t st) {
@@ -239,7 +265,7 @@ void launch_win_prep_bwd(const WinPrep &q, const WinBwdPrep &b, int grid_kv, hip
   const unsigned item_blocks = q.n_q * (int64_t)q.h_q <= kWinAlonePairs ? 1 : prep_blocks(q);
   hipLaunchKernelGGL(win_tiles_kernel, dim3(item_blocks + (unsigned)b.T), dim3(kPrepThreads), 0,
                      st, q, b, item_blocks);
-  const int64_t places = b.n_blocks * b.h_kv / kPrepThreads + 1;
+  const int64_t places = b.parts > 1 ? 1 : b.n_blocks * b.h_kv / kPrepThreads + 1;
   hipLaunchKernelGGL(win_kv_items_kernel, dim3(1 + (unsigned)(places < 128 ? places : 128)),
                      dim3(kPrepThreads), 0, st, b);
 }

@@ -69,7 +69,8 @@ def attention(q, k, v, ok, cov, scale=None, dout=None, held=None):
     G = h_q // h_kv
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     q, k, v = q.double(), k.double(), v.double()
-    z = dict(dtype=torch.float64)
+    ok, cov = ok.to(q.device), cov.to(q.device)
+    z = dict(dtype=torch.float64, device=q.device)
     O, Ob = torch.zeros((n_q, h_q, d), **z), torch.zeros((n_q, h_q, d), **z)
     LSE = torch.zeros((h_q, n_q), **z)
     if dout is not None:
@@ -119,7 +120,7 @@ def attention(q, k, v, ok, cov, scale=None, dout=None, held=None):
 
 def close(name, got, ref, where=None):
     """``got`` within the bound of ``ref`` (value, bound); bf16 dK and dV get their rounding."""
-    value, bound = ref
+    value, bound = (x.cpu() for x in ref)
     got = got.detach().cpu()
     if got.dtype == torch.bfloat16 and name in ("dk", "dv"):
         bound = bound + HALF * value.abs()
