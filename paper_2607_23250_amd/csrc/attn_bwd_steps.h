@@ -42,7 +42,7 @@ struct KvShape {
 //
 // LANES: the lanes of the wave look at 64 tiles at once for the next one with rows of the
 // item.  A windowed item meets few of its candidates, and one tile after another cost up
-// to 0.5 us each (the far rows of a 16K sample, 16 tiles x 2 head shards: 159 us, [SINK] with
+// to 0.5 us each (the far rows of a 16K sample, 16 tiles x 2 head shards: 159 us, 145 with
 // this search).
 template <bool LANES>
 struct StepIter {

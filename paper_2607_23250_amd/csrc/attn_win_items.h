@@ -154,11 +154,11 @@ __device__ __forceinline__ void for_each_win_item(const WinTile &t, int64_t wa,
 }
 
 // ---------------------------------------------------------------------------
-// Calls of single tokens (no more Q rows than tiles): no list.  Unit (tile, head chunk, part)
-// finds its work itself, which saves the preparation's launch and most of its time (64
-// sequences, 32 / 8 heads: 20 of 239 us; one: 11 of 25).  A tile of one row has one item of
-// each chunk, cut into up to `parts` key ranges of equal length; of a tile with more rows (the
-// rule allows them) unit p takes every parts-th 32-row window, and its items stay whole.
+// Calls of single tokens (no more Q rows than tiles) and small ones: no list.  Unit (tile, head
+// chunk, part) finds its work itself, which saves the preparation's launch and most of its time
+// (64 sequences, 32 / 8 heads: 20 of 239 us; one: 11 of 25).  Unit p of a tile of one row has
+// key range p of up to `cuts` of equal length of its item; of a tile with more rows it has every
+// parts-th 32-row window from window p on, and whole items.
 struct WinRows {
   const int64_t *cu;
   int64_t n;
@@ -170,11 +170,13 @@ struct WinRows {
   int32_t *hdr;
   int chunks;   // head chunks of all heads
   int parts;    // units of a tile and chunk
+  int cuts;     // key ranges of a single row's item at most
   int64_t units() const { return T * chunks * parts; }
 };
-// Parts of an item of this many steps.
-__device__ __forceinline__ int row_parts(int steps, int parts) {
-  return max(1, min(parts, steps / kWinMinSteps));
+constexpr int kRowMinSteps = 2;   // a key range of a single row walks at least 2 key blocks
+// Key ranges of a single row's item of this many steps.
+__device__ __forceinline__ int row_parts(int steps, int cuts) {
+  return max(1, min(cuts, steps / kRowMinSteps));
 }
 // Last sample that begins at or before x (uniform in the wave): guess, then 64-ary search.
 __device__ __forceinline__ int64_t sample_at(const int64_t *cu, int64_t n, int64_t x,
@@ -238,13 +240,13 @@ struct RowUnit {
         if (pb + rb >= (wb < pe ? wb : pe)) continue;
         it = win_item(t, c0, pb, pe, rb, 1 << sh, g, h0, nh, a.win);
         if (!one_row()) return true;
-        const int np = row_parts(it.kb1, a.parts), per = (it.kb1 + np - 1) / np;
+        const int np = row_parts(it.kb1, a.cuts), per = (it.kb1 + np - 1) / np;
         valid = false;   // the only one
-        if (p * per >= it.kb1) return false;
+        if (p * per >= it.kb1) return false;   // per <= kb1: parts past the cuts have none
         if (np > 1) {
           it.kb0 = p * per;
           it.kb1 = min((p + 1) * per, it.kb1);
-          it.slot = (int32_t)(job * a.parts + p);
+          it.slot = (int32_t)(job * a.cuts + p);
         }
         return true;
       }
@@ -544,6 +546,8 @@ inline bool win_may_split(const Window &w, int64_t n_kv) {
 }
 // Single tokens beyond this many (tile, head chunk) pairs go through the list.
 constexpr int64_t kMaxRowJobs = 1 << 20;
+// Other calls without a list have at most this many units.
+constexpr int64_t kMaxSmallUnits = 4096;
 
 // Arguments of the windowed dQ kernel (attn_window_dq.hip).  q and o, or q8 and o8.
 struct WinDq {

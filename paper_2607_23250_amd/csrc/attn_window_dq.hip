@@ -101,17 +101,23 @@ __global__ __launch_bounds__(kThreads, 2) void win_dq_kernel(WinDq a) {
       const bf16 *base = (part ? a.v : a.k) + ((size_t)(key0 + kb) * h_kv + it.g) * D;
       const uint32_t ld = lds_addr(smem + buf * S::STAGE + part * S::K_EL) + 1024u * w;
       constexpr uint32_t e = kWaves * 1024u;
-      uint32_t at[S::NK];
-      static_for<S::NK>([&](auto u) {
-        const int r = swu_row<S::KC>(w + kWaves * u, l);
-        at[u] = last >= kFwdBN - 1 ? k_lane[u]
-                                   : k_lane[u] - 2u * (uint32_t)(max(r - last, 0) * h_kv * D);
-      });
-      if constexpr (S::NK == 4) {
-        g2l16x4r(base, at[0], at[1], at[2], at[3], ld, ld + e, ld + 2 * e, ld + 3 * e);
+      auto copy = [&](const uint32_t (&at)[S::NK]) {
+        if constexpr (S::NK == 4) {
+          g2l16x4r(base, at[0], at[1], at[2], at[3], ld, ld + e, ld + 2 * e, ld + 3 * e);
+        } else {
+          g2l16s(base, at[0], ld);
+          g2l16s(base, at[1], ld + e);
+        }
+      };
+      if (__builtin_expect(last >= kFwdBN - 1, 1)) {
+        copy(k_lane);
       } else {
-        g2l16s(base, at[0], ld);
-        g2l16s(base, at[1], ld + e);
+        uint32_t at[S::NK];
+        static_for<S::NK>([&](auto u) {
+          const int r = swu_row<S::KC>(w + kWaves * u, l);
+          at[u] = k_lane[u] - 2u * (uint32_t)(max(r - last, 0) * h_kv * D);
+        });
+        copy(at);
       }
     };
     issue(kb0, 0, 0);
@@ -173,13 +179,12 @@ __global__ __launch_bounds__(kThreads, 2) void win_dq_kernel(WinDq a) {
     f32x16 acc[NT];
     static_for<NT>([&](auto dt) { acc[dt] = mfma_zero_c(); });
     float d_run = 0.f;      // this lane's sum of dS over its keys
-    const int seen = min(win.sinks, qloc + 1);   // keys below: visible sinks
     wait_vm_known();   // no wait for the rows inside the loop
     __syncthreads();
 
     for (int b = kb0; b < nkb; ++b) {
       const int buf = (b - kb0) & 1;
-      const bool more = b + 1 < nkb;
+      const bool more = __builtin_expect(b + 1 < nkb, 1);
       const int kb = step_block(b, it.far, it.gap) * kFwdBN;
       const bf16 *Ks = smem + buf * S::STAGE;
       bf16x8 dsf[2][2];   // dS^T of the halves (B operands, two 16-key chunks)
@@ -203,12 +208,22 @@ __global__ __launch_bounds__(kThreads, 2) void win_dq_kernel(WinDq a) {
           __builtin_amdgcn_sched_barrier(0);
         });
         if (copy) issue(b + 1, buf ^ 1, 0);
+        // keys that a row does not attend, as in the forward
         const int k0 = kb + 32 * H;
-        // some row of the wave does not attend all of the half's keys
-        if (k0 <= qlast - win.size || k0 + 31 > qmin) {
+        int hi = qloc - k0 - 8 * kg;
+        if (__builtin_expect(k0 + 31 > qmin, 0)) {
+          asm volatile("" : "+v"(hi));
           static_for<16>([&](auto r) {
-            const int kl = k0 + 16 * (r >> 3) + 8 * kg + (r & 7);
-            if ((uint32_t)(qloc - kl) >= (uint32_t)win.size && kl >= seen) sa[int(r)] = -INFINITY;
+            constexpr int at = 16 * (r >> 3) + (r & 7);
+            sa[int(r)] = at > hi ? -INFINITY : sa[int(r)];
+          });
+        }
+        if (__builtin_expect(k0 <= qlast - win.size, 0)) {
+          int sk = max(win.sinks - k0 - 8 * kg, 0), gone = max(hi - win.size + 1 - sk, 0);
+          asm volatile("" : "+v"(sk), "+v"(gone));
+          static_for<16>([&](auto r) {
+            constexpr int at = 16 * (r >> 3) + (r & 7);
+            sa[int(r)] = (uint32_t)(at - sk) < (uint32_t)gone ? -INFINITY : sa[int(r)];
           });
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -257,11 +272,11 @@ __global__ __launch_bounds__(kThreads, 2) void win_dq_kernel(WinDq a) {
       };
       const bool u0 = used(kb), u1 = used(kb + 32);
       // one place for each: accumulators that came from several would be copied
-      if (u0) half(H0{}, more);
+      if (__builtin_expect(u0, 1)) half(H0{}, more);
       else if (more) issue(b + 1, buf ^ 1, 0), issue(b + 1, buf ^ 1, 1);
-      if (u1) half(H1{}, false);
-      if (u0) add(H0{});
-      if (u1) add(H1{});
+      if (__builtin_expect(u1, 1)) half(H1{}, false);
+      if (__builtin_expect(u0, 1)) add(H0{});
+      if (__builtin_expect(u1, 1)) add(H1{});
       wait_vm();
       __syncthreads();
     }

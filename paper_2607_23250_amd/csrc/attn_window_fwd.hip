@@ -67,8 +67,8 @@ struct NoUnit {
   __device__ __forceinline__ NoUnit(const NoRows &, int64_t) {}
 };
 
-// R: NoRows (the items of the list) or WinRows (single tokens: the workgroup's items are those
-// of one unit; the last workgroup counts the tiles outside the buffers instead).
+// R: NoRows (the items of the list) or WinRows (no list: the workgroup's items are those of
+// one unit; the last workgroup counts the tiles outside the buffers instead).
 template <int D, typename R>
 __global__ __launch_bounds__(kThreads, (kWinFwdPerCu<D, std::is_same_v<R, WinRows>>)) void
 win_fwd_kernel(WinFwd a, R rows) {
@@ -137,17 +137,23 @@ win_fwd_kernel(WinFwd a, R rows) {
     const bf16 *base = (part ? a.v : a.k) + ((size_t)(x.sample + kb) * h_kv + x.g) * D;
     const uint32_t ld = lds_addr(smem + buf * S::STAGE + part * S::K_EL) + 1024u * w;
     constexpr uint32_t e = kWaves * 1024u;
-    uint32_t at[S::NK];
-    static_for<S::NK>([&](auto u) {
-      const int r = swu_row<S::KC>(w + kWaves * u, l);
-      at[u] = last >= kFwdBN - 1 ? k_lane[u]
-                                 : k_lane[u] - 2u * (uint32_t)(max(r - last, 0) * h_kv * D);
-    });
-    if constexpr (S::NK == 4) {
-      g2l16x4r(base, at[0], at[1], at[2], at[3], ld, ld + e, ld + 2 * e, ld + 3 * e);
+    auto copy = [&](const uint32_t (&at)[S::NK]) {
+      if constexpr (S::NK == 4) {
+        g2l16x4r(base, at[0], at[1], at[2], at[3], ld, ld + e, ld + 2 * e, ld + 3 * e);
+      } else {
+        g2l16s(base, at[0], ld);
+        g2l16s(base, at[1], ld + e);
+      }
+    };
+    if (__builtin_expect(last >= kFwdBN - 1, 1)) {
+      copy(k_lane);
     } else {
-      g2l16s(base, at[0], ld);
-      g2l16s(base, at[1], ld + e);
+      uint32_t at[S::NK];
+      static_for<S::NK>([&](auto u) {
+        const int r = swu_row<S::KC>(w + kWaves * u, l);
+        at[u] = k_lane[u] - 2u * (uint32_t)(max(r - last, 0) * h_kv * D);
+      });
+      copy(at);
     }
   };
   // an item's first block, and this lane's query row
@@ -188,20 +194,19 @@ win_fwd_kernel(WinFwd a, R rows) {
     f32x16 oacc[NT];
     static_for<NT>([&](auto dt) { oacc[dt] = mfma_zero_c(); });
     float m_run = -INFINITY, l_run = 0.f;
-    const int seen = min(win.sinks, qloc + 1);   // keys below: visible sinks
     for (int b = kb0; b < nkb; ++b) {
       const int buf = (b - kb0) & 1;
-      const bool more = b + 1 < nkb;
+      const bool more = __builtin_expect(b + 1 < nkb, 1);
       const int kb = step_block(b, it.far, it.gap) * kFwdBN;
       const bf16 *Ks = smem + buf * S::STAGE, *Vs = Ks + S::K_EL;
       // does some row of the wave attend a key of the half that begins at k0?
       auto used = [&](int k0) {
         return b < pend && k0 <= qlast && (k0 + 31 > qmin - win.size || k0 < win.sinks);
       };
-      const bool u0 = used(kb), u1 = used(kb + 32);
+      const bool u0 = __builtin_expect(used(kb), 1), u1 = __builtin_expect(used(kb + 32), 1);
       // the next block's K rows after this one's S^T products, its V rows after the softmax
       // (a wave without keys in this block posts both at once)
-      if (!u0 && !u1) {
+      if (__builtin_expect(!u0 && !u1, 0)) {
         if (more) {
           issue(it, b + 1, buf ^ 1, 0);
           issue(it, b + 1, buf ^ 1, 1);
@@ -226,21 +231,9 @@ win_fwd_kernel(WinFwd a, R rows) {
             __builtin_amdgcn_sched_barrier(0);
           });
         };
-        // the keys of a half that a row does not attend
-        auto mask = [&](auto h_t) {
-          constexpr int H = decltype(h_t)::value;
-          const int k0 = kb + 32 * H;
-          if (k0 <= qlast - win.size || k0 + 31 > qmin) {
-            static_for<16>([&](auto r) {
-              const int kl = k0 + 16 * (r >> 3) + 8 * kg + (r & 7);
-              if ((uint32_t)(qloc - kl) >= (uint32_t)win.size && kl >= seen)
-                s[H][int(r)] = -INFINITY;
-            });
-          }
-        };
         using H0 = std::integral_constant<int, 0>;
         using H1 = std::integral_constant<int, 1>;
-        if (u0) {
+        if (__builtin_expect(u0, 1)) {
           static_for<AHEAD>([&](auto i) { rd(i); });
           __builtin_amdgcn_sched_barrier(0);
           score(H0{});
@@ -248,11 +241,33 @@ win_fwd_kernel(WinFwd a, R rows) {
           static_for<AHEAD>([&](auto i) { rd(std::integral_constant<int, NC + i>{}); });
           static_for<16>([&](auto r) { s[0][int(r)] = -INFINITY; });
         }
-        if (u1) score(H1{});
+        if (__builtin_expect(u1, 1)) score(H1{});
         else static_for<16>([&](auto r) { s[1][int(r)] = -INFINITY; });
         if (more) issue(it, b + 1, buf ^ 1, 0);
-        if (u0) mask(H0{});
-        if (u1) mask(H1{});
+        // Keys that a row does not attend, by their place `at` in the block (less 8 kg): those
+        // after the row, at > hi; and from the sinks' end to the window's start, at in
+        // [sk, sk + gone).  The empty asm keeps the comparisons in their branch: taken out of it,
+        // they need more scalar registers than there are.
+        int hi = qloc - kb - 8 * kg;
+        if (__builtin_expect(kb + kFwdBN - 1 > qmin, 0)) {
+          asm volatile("" : "+v"(hi));
+          static_for<2>([&](auto t) {
+            static_for<16>([&](auto r) {
+              constexpr int at = 32 * t + 16 * (r >> 3) + (r & 7);
+              s[t][int(r)] = at > hi ? -INFINITY : s[t][int(r)];
+            });
+          });
+        }
+        if (__builtin_expect(kb <= qlast - win.size, 0)) {
+          int sk = max(win.sinks - kb - 8 * kg, 0), gone = max(hi - win.size + 1 - sk, 0);
+          asm volatile("" : "+v"(sk), "+v"(gone));
+          static_for<2>([&](auto t) {
+            static_for<16>([&](auto r) {
+              constexpr int at = 32 * t + 16 * (r >> 3) + (r & 7);
+              s[t][int(r)] = (uint32_t)(at - sk) < (uint32_t)gone ? -INFINITY : s[t][int(r)];
+            });
+          });
+        }
         // P with the running max, which moves only when the block's row sum of P exceeds
         // 256 (as in the causal forward)
         bf16x8 pf[4];
@@ -272,7 +287,7 @@ win_fwd_kernel(WinFwd a, R rows) {
           expo(-m_run);
           move = !(row_sum2(ps) <= 256.f);
         }
-        if (__builtin_amdgcn_ballot_w64(move)) {
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(move) != 0, 0)) {
           float mx = -INFINITY;
           static_for<2>([&](auto t) {
             static_for<16>([&](auto r) { mx = fmaxf(mx, s[t][int(r)]); });
@@ -304,12 +319,12 @@ win_fwd_kernel(WinFwd a, R rows) {
             __builtin_amdgcn_sched_barrier(0);
           });
         };
-        if (u0) static_for<AHEAD>([&](auto j) { rt(j); });
+        if (__builtin_expect(u0, 1)) static_for<AHEAD>([&](auto j) { rt(j); });
         else static_for<AHEAD>([&](auto j) { rt(std::integral_constant<int, NQ + j>{}); });
         if (more) issue(it, b + 1, buf ^ 1, 1);
         __builtin_amdgcn_sched_barrier(0);
-        if (u0) add(H0{});
-        if (u1) add(H1{});
+        if (__builtin_expect(u0, 1)) add(H0{});
+        if (__builtin_expect(u1, 1)) add(H1{});
       }
       wait_vm();
       __syncthreads();
@@ -419,10 +434,27 @@ static int reserve_lds() {
   return LIBRA_OK;
 }
 
-// Single tokens: no more Q rows than tiles, and not more (tile, head chunk) pairs than a
-// grid of them should have.
-static bool single_tokens(const WinRows &r) {
-  return r.n_q <= r.T && r.T * r.chunks <= kMaxRowJobs;
+// How a call without a list runs (parts, cuts); false: it has one.
+//   * Single tokens, no more Q rows than tiles: up to eight units for each CU, one for each key
+//     range, as long as the slots of their partial results suffice.
+//   * Small calls whose items are too short to be cut: as many units as the longest tile that
+//     the rows allow has windows, so that none has two (512 tokens, 8 / 2 heads, window 128:
+//     16.6 us with a list, 9.9 without).
+static bool without_list(WinRows &r, int max_parts, int cus) {
+  const int64_t jobs = r.T * r.chunks;
+  const int64_t steps = win_max_steps(r.win, r.n_kv);
+  if (r.n_q <= r.T && jobs <= kMaxRowJobs) {
+    const int64_t most = std::min<int64_t>(steps / kRowMinSteps, max_parts / jobs);
+    r.cuts = r.parts =
+        (int)std::max<int64_t>(1, std::min<int64_t>(most, 8 * (int64_t)cus / jobs));
+    return true;
+  }
+  const int64_t windows = (r.n_q + kRows - 1) / kRows;
+  if (win_may_split(r.win, r.n_kv) || jobs > kMaxSmallUnits || jobs * windows > kMaxSmallUnits)
+    return false;
+  r.parts = (int)windows;
+  r.cuts = 1;
+  return true;
 }
 
 template <int D>
@@ -432,20 +464,14 @@ static int launch_win_fwd_d(const WinFwd &a, WinRows rows, const FwdLayout &L, F
   int dev = 0, cus = 256;
   hipGetDevice(&dev);
   hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
-  if (single_tokens(rows)) {
-    // eight units for each CU, if the slots of their parts suffice; parts of kWinMinSteps
-    // blocks at least
-    const int64_t jobs = rows.T * rows.chunks;
-    const int64_t most = std::min<int64_t>(win_max_steps(a.win, rows.n_kv) / kWinMinSteps,
-                                           L.max_parts / jobs);
-    rows.parts = (int)std::max<int64_t>(1, std::min<int64_t>(most, 8 * (int64_t)cus / jobs));
+  if (without_list(rows, L.max_parts, cus)) {
     if (int rc = reserve_lds<D, WinRows>()) return rc;
     if (tm) hipEventRecord(tm->begin, st);
     hipLaunchKernelGGL(HIP_KERNEL_NAME(win_fwd_kernel<D, WinRows>),
                        dim3((unsigned)(rows.units() + 1)), dim3(kThreads), S::SMEM, st, a, rows);
-    if (rows.parts > 1)
-      hipLaunchKernelGGL(win_rows_combine_kernel<D>, dim3((unsigned)jobs), dim3(256), 0, st, rows,
-                         a.parts, a.o, a.lse);
+    if (rows.cuts > 1)
+      hipLaunchKernelGGL(win_rows_combine_kernel<D>, dim3((unsigned)(rows.T * rows.chunks)),
+                         dim3(256), 0, st, rows, a.parts, a.o, a.lse);
   } else {
     if (int rc = reserve_lds<D, NoRows>()) return rc;
     const int grid = cus * kWinFwdPerCu<D, false>;
@@ -476,7 +502,7 @@ int launch_win_fwd(const void *q, const void *k, const void *v, const int64_t *c
                  hdr, h_q, h_kv, n_q, scale * kLog2e, static_cast<bf16 *>(o), lse,
                  reinterpret_cast<float *>(W + L.parts), win};
   const WinRows rows{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, win, hdr,
-                     h_kv * ((h_q / h_kv + 3) / 4), 1};
+                     h_kv * ((h_q / h_kv + 3) / 4), 1, 1};
   auto *splits = reinterpret_cast<FwdSplit *>(W + L.splits);
   return (d == 128 ? launch_win_fwd_d<128> : launch_win_fwd_d<64>)(a, rows, L, splits, st, tm);
 }
