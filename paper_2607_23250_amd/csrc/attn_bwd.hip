@@ -506,10 +506,8 @@ __device__ __forceinline__ void absmax_q(unsigned block, unsigned split,
     const int64_t row = m * kRows + r;
     const bool ok = row >= ra && row < rb && !(WIN && row >= past);
     if constexpr (WIN) {
-      // several heads' loads at once: the pass is bound by them (537 MB of Q and dO with
-      // 153 us one head at a time)
+      // bound by memory: 805 MB of Q, dO, K and V and of zeroed gradients in 155 us
       if (ok) {
-#pragma unroll 4
         for (int h = tl.head_begin; h < tl.head_end; ++h) {
           const size_t off = ((size_t)row * h_q + h) * D + part * (D / 8);
           static_for<D / 64>([&](auto c) {
@@ -727,7 +725,8 @@ __global__ __launch_bounds__(256) void bwd_max_kernel(BwdPass a) {
     kv_pass<D, false, WIN>(b, a.kv_blocks, a.k, a.v, a.cu, a.n, a.ext, a.h_kv, a.n_kv, a.hdr,
                            a.k16, a.v16, a.win);
   } else if ((b -= a.kv_blocks) < a.tile_blocks) {
-    absmax_q<D, WIN, HELD>(b, WIN ? a.tile_split : kTileSplit, a.q, a.q8, a.dout, a.tiles, a.h_q, a.n_q, a.n_kv, a.cu[a.n], a.hdr, a.rec);
+    absmax_q<D, WIN, HELD>(b, WIN ? a.tile_split : kTileSplit, a.q, a.q8, a.dout, a.tiles, a.h_q,
+                           a.n_q, a.n_kv, a.cu[a.n], a.hdr, a.rec);
   } else {
     b -= a.tile_blocks;
     const unsigned half = a.zero_blocks / 2;
@@ -1345,14 +1344,7 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
   f16 *v16 = reinterpret_cast<f16 *>(ws + L.v16);
   float *stats = reinterpret_cast<float *>(ws + L.stats);
   int32_t *cov = reinterpret_cast<int32_t *>(ws + L.cov);
-  static bool attr_set = false;
-  if (!attr_set) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_bwd_dkdv_kernel<D, WIN>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize,
-                            (int)KvShape<D>::SMEM) != hipSuccess)
-      return fail(LIBRA_EHIP, "hipFuncSetAttribute failed");
-    attr_set = true;
-  }
+  if (int rc = reserve_lds<&attn_bwd_dkdv_kernel<D, WIN>>(KvShape<D>::SMEM)) return rc;
   // bf16 dK / dV are written where a covered row attends and zero elsewhere
   const int64_t n16 = accumulate ? 0 : n_kv * h_kv * D * (int64_t)sizeof(bf16) / 16;
   const unsigned zero_blocks = (unsigned)std::min<int64_t>((n16 + 255) / 256, 4096);
@@ -1386,7 +1378,7 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
                       win_kv_parts(win, L.max_blocks / h_kv, h_kv, cus)};
       launch_win_prep_bwd(WinPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, win, hdr, qitems,
                                   L.max_qitems, 0, cus * kWinDqPerCu, cus * kWinDqPerCu,
-                                  max_parts, 0, splits}, wb, cus, st);
+                                  max_parts, splits}, wb, cus, st);
     } else {
       max_parts = may_split(n_kv) ? L.max_parts : 0;
       hipLaunchKernelGGL(prep_bwd_kernel, dim3(2), dim3(kPrepThreads), 0, st,

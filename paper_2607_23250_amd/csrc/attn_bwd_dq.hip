@@ -434,13 +434,7 @@ static int launch_dq(const bf16 *q, const bf16 *dout, const bf16 *k, const bf16 
                      bf16 *dq, f16 *rec, const FwdSplit *splits, float *parts, int max_parts,
                      int blocks, hipStream_t st, const KernelTimer *tm, float d_fix) {
   constexpr size_t smem = DqShape<D>::SMEM;
-  static bool attr_set = false;
-  if (!attr_set) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_bwd_dq_kernel<D>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != hipSuccess)
-      return fail(LIBRA_EHIP, "cannot reserve %zu bytes of LDS for the dQ kernel", smem);
-    attr_set = true;
-  }
+  if (int rc = reserve_lds<&attn_bwd_dq_kernel<D>>(smem)) return rc;
   if (tm) hipEventRecord(tm->begin, st);
   hipLaunchKernelGGL(attn_bwd_dq_kernel<D>, dim3(blocks), dim3(2 * kThreads), smem, st, q, dout, k,
                      v, stats, cu, items, hdr, h_q, h_kv, n_q, n_kv, nq_pad, scale * kLog2e, scale,

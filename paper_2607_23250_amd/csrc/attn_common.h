@@ -3,9 +3,11 @@
 
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 #include <type_traits>
 
+#include "errors.h"
 #include "libra.h"
 
 namespace libra {
@@ -787,5 +789,20 @@ int launch_bwd(const void *q, const void *k, const void *v, const void *o, const
                bool exact_o = true,   // see d_fix of the dQ kernel
                const Window &win = {},
                const Held &q8 = {}, const Held &o8 = {});   // windowed: q and o, if q and o are null
+
+// Lets Kernel have `bytes` of dynamic LDS on the current device (asked for once on each).
+template <auto Kernel>
+int reserve_lds(size_t bytes) {
+  static std::atomic<uint64_t> done{0};   // a bit for each of the first 64 devices
+  int dev = 0;
+  hipGetDevice(&dev);
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return LIBRA_OK;
+  if (hipFuncSetAttribute(reinterpret_cast<const void *>(Kernel),
+                          hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess)
+    return fail(LIBRA_EHIP, "cannot reserve %zu bytes of LDS", bytes);
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return LIBRA_OK;
+}
 
 }  // namespace libra

@@ -411,14 +411,7 @@ static int launch_fwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const int64
   FwdItem *items = reinterpret_cast<FwdItem *>(ws + L.items);
   auto *splits = reinterpret_cast<FwdSplit *>(ws + L.splits);
   float *parts = reinterpret_cast<float *>(ws + L.parts);
-  static bool attr_set = false;
-  if (!attr_set) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_fwd_kernel<D>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize,
-                            (int)FwdShape<D>::SMEM) != hipSuccess)
-      return fail(LIBRA_EHIP, "hipFuncSetAttribute failed");
-    attr_set = true;
-  }
+  if (int rc = reserve_lds<&attn_fwd_kernel<D>>(FwdShape<D>::SMEM)) return rc;
   int dev = 0, cus = 256;
   hipGetDevice(&dev);
   hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);

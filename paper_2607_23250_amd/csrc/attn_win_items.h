@@ -37,7 +37,7 @@ struct WinPrep {
   int count_bad;
   int grid;        // workgroups that run the items
   int split_grid;  // workgroups that the split rule counts
-  int max_parts, idle_only;
+  int max_parts;   // 0: no item is split
   FwdSplit *splits;
 };
 constexpr int kWinMinSteps = 4;   // a part of a split item walks at least 4 key blocks
@@ -275,11 +275,10 @@ __device__ __forceinline__ void clear_win_header(int32_t *hdr, int grid_q, int64
 // One workgroup (gridDim.x = 1, or workgroup 0 when the tiles turn out to cover few
 // rows) or many, each with an equal run of the units (tile, head chunk, 32-row window).
 //
-// Split K: a call with fewer items than twice `split_grid` (with `idle_only`, only if
-// whole rounds of them would leave more than a tenth of the workgroups idle) cuts items
-// of at least two parts into key ranges of about a quarter of a workgroup's share, as
-// the causal calls do; one workgroup then builds the list, and the parts' slots go by
-// its order, so that nothing depends on which part runs where.
+// Split K: a call with fewer items than twice `split_grid` cuts items of at least two parts
+// into key ranges of about a quarter of a workgroup's share, as the causal calls do; one
+// workgroup then builds the list, and the parts' slots go by its order, so that nothing
+// depends on which part runs where.
 __device__ __forceinline__ void prep_win(const WinPrep &a, WinPrepLds &lds, unsigned block,
                                          unsigned blocks) {
   const int tid = threadIdx.x, l = tid & 63, G = a.h_q / a.h_kv;
@@ -400,8 +399,7 @@ __device__ __forceinline__ void prep_win(const WinPrep &a, WinPrepLds &lds, unsi
     });
     __syncthreads();
     const unsigned long long items = lds.items, work = lds.work, gr = (unsigned)a.split_grid;
-    const bool idle = items * 10 < (items + gr - 1) / gr * gr * 9;
-    if (items > 0 && items < 2 * gr && (idle || !a.idle_only)) {
+    if (items > 0 && items < 2 * gr) {
       // items longer than C number at most work / C, their parts at most twice that
       const unsigned long long c = (work + 4 * gr - 1) / (4 * gr);
       const unsigned long long fit = (2 * work + a.max_parts - 1) / (unsigned)a.max_parts;

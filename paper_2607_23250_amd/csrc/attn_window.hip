@@ -455,14 +455,7 @@ __global__ __launch_bounds__(256) void win_sink_sum_kernel(const WinSink *__rest
 template <int D>
 static int launch_sinks(const f16 *k16, const f16 *v16, const f16 *rec, const WinBwdPrep &b,
                         float c2, float *parts, int cus, hipStream_t st) {
-  static bool attr_set = false;
-  if (!attr_set) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(&win_sink_kernel<D>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize,
-                            (int)KvShape<D>::SMEM) != hipSuccess)
-      return fail(LIBRA_EHIP, "hipFuncSetAttribute failed");
-    attr_set = true;
-  }
+  if (int rc = reserve_lds<&win_sink_kernel<D>>(KvShape<D>::SMEM)) return rc;
   hipLaunchKernelGGL(win_sink_kernel<D>, dim3(cus), dim3(kThreads), KvShape<D>::SMEM, st, k16,
                      v16, rec, b, c2, parts);
   hipLaunchKernelGGL(win_sink_sum_kernel<D>, dim3(cus * 2), dim3(256), 0, st, b.sinks, b.hdr,

@@ -333,14 +333,7 @@ __global__ __launch_bounds__(kThreads, 2) void win_dq_kernel(WinDq a) {
 
 template <int D, bool HELD>
 static int launch(const WinDq &a, int cus, hipStream_t st) {
-  static bool attr_set = false;
-  if (!attr_set) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(&win_dq_kernel<D, HELD>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize,
-                            (int)WinDqShape<D>::SMEM) != hipSuccess)
-      return fail(LIBRA_EHIP, "hipFuncSetAttribute failed");
-    attr_set = true;
-  }
+  if (int rc = reserve_lds<&win_dq_kernel<D, HELD>>(WinDqShape<D>::SMEM)) return rc;
   hipLaunchKernelGGL(HIP_KERNEL_NAME(win_dq_kernel<D, HELD>), dim3(cus * kWinDqPerCu),
                      dim3(kThreads), WinDqShape<D>::SMEM, st, a);
   return LIBRA_OK;

@@ -10,7 +10,7 @@
 //     masked key at all);
 //   * a half that some row does not attend whole is masked by element, and a row may have no
 //     key in it, so the running max starts at the lowest finite value;
-//   * keys past the item's last row are not read: in a cache they may hold anything.
+//   * keys that no row of the item attends are not read: in a cache they may hold anything.
 // Bound by the matrix cores for long windows; single tokens (WinRows) by reading K and V.
 #include <hip/hip_runtime.h>
 
@@ -129,11 +129,12 @@ win_fwd_kernel(WinFwd a, R rows) {
       return true;
     }
   };
-  // global -> LDS, asynchronous: the K (part 0) or V (part 1) rows of step b of an item; keys
-  // past its last row read that row's key
+  // global -> LDS, asynchronous: the K (part 0) or V (part 1) rows of step b of an item.  In
+  // the place of a key that none of its rows attends (past the last row, or between the sinks
+  // and the window of the first row) one is read that some row does.
   auto issue = [&](const FwdItem &x, int b, int buf, int part) {
     const int kb = step_block(b, x.far, x.gap) * kFwdBN;
-    const int last = x.q_loc0 + x.nrows - 1 - kb;
+    const int last = x.q_loc0 + x.nrows - 1 - kb;   // the last row's key in the block
     const bf16 *base = (part ? a.v : a.k) + ((size_t)(x.sample + kb) * h_kv + x.g) * D;
     const uint32_t ld = lds_addr(smem + buf * S::STAGE + part * S::K_EL) + 1024u * w;
     constexpr uint32_t e = kWaves * 1024u;
@@ -145,13 +146,18 @@ win_fwd_kernel(WinFwd a, R rows) {
         g2l16s(base, at[1], ld + e);
       }
     };
-    if (__builtin_expect(last >= kFwdBN - 1, 1)) {
+    if (__builtin_expect(b > x.far && last >= kFwdBN - 1, 1)) {
       copy(k_lane);
     } else {
+      // the first row's window begins at `from`, the sinks end at sk
+      int from = x.q_loc0 - win.size + 1 - kb, sk = win.sinks - kb;
+      asm volatile("" : "+v"(from), "+v"(sk));
       uint32_t at[S::NK];
       static_for<S::NK>([&](auto u) {
         const int r = swu_row<S::KC>(w + kWaves * u, l);
-        at[u] = k_lane[u] - 2u * (uint32_t)(max(r - last, 0) * h_kv * D);
+        int key = min(r, last);
+        if (key >= sk && key < from) key = from < kFwdBN ? from : sk - 1;
+        at[u] = k_lane[u] + 2u * (uint32_t)((key - r) * h_kv * D);
       });
       copy(at);
     }
@@ -421,19 +427,6 @@ __global__ __launch_bounds__(256) void win_rows_combine_kernel(WinRows a,
     lse[(size_t)head * a.n_q + it.q_row0] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-template <int D, typename R>
-static int reserve_lds() {
-  static bool attr_set = false;
-  if (!attr_set) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(&win_fwd_kernel<D, R>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize,
-                            (int)WinFwdShape<D>::SMEM) != hipSuccess)
-      return fail(LIBRA_EHIP, "hipFuncSetAttribute failed");
-    attr_set = true;
-  }
-  return LIBRA_OK;
-}
-
 // How a call without a list runs (parts, cuts); false: it has one.
 //   * Single tokens, no more Q rows than tiles: up to eight units for each CU, one for each key
 //     range, as long as the slots of their partial results suffice.
@@ -465,7 +458,7 @@ static int launch_win_fwd_d(const WinFwd &a, WinRows rows, const FwdLayout &L, F
   hipGetDevice(&dev);
   hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
   if (without_list(rows, L.max_parts, cus)) {
-    if (int rc = reserve_lds<D, WinRows>()) return rc;
+    if (int rc = reserve_lds<&win_fwd_kernel<D, WinRows>>(S::SMEM)) return rc;
     if (tm) hipEventRecord(tm->begin, st);
     hipLaunchKernelGGL(HIP_KERNEL_NAME(win_fwd_kernel<D, WinRows>),
                        dim3((unsigned)(rows.units() + 1)), dim3(kThreads), S::SMEM, st, a, rows);
@@ -473,12 +466,12 @@ static int launch_win_fwd_d(const WinFwd &a, WinRows rows, const FwdLayout &L, F
       hipLaunchKernelGGL(win_rows_combine_kernel<D>, dim3((unsigned)(rows.T * rows.chunks)),
                          dim3(256), 0, st, rows, a.parts, a.o, a.lse);
   } else {
-    if (int rc = reserve_lds<D, NoRows>()) return rc;
+    if (int rc = reserve_lds<&win_fwd_kernel<D, NoRows>>(S::SMEM)) return rc;
     const int grid = cus * kWinFwdPerCu<D, false>;
     const int max_parts = win_may_split(a.win, rows.n_kv) ? L.max_parts : 0;
     launch_win_prep_fwd(WinPrep{rows.cu, rows.n, rows.tiles, rows.T, rows.h_q, rows.h_kv, rows.n_q,
                                 rows.n_kv, a.win, a.hdr, const_cast<FwdItem *>(a.items),
-                                L.max_items, 1, grid, cus * 2, max_parts, 0, splits}, st);
+                                L.max_items, 1, grid, cus * 2, max_parts, splits}, st);
     if (tm) hipEventRecord(tm->begin, st);
     hipLaunchKernelGGL(HIP_KERNEL_NAME(win_fwd_kernel<D, NoRows>), dim3(grid), dim3(kThreads),
                        S::SMEM, st, a, NoRows{});

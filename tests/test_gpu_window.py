@@ -284,6 +284,31 @@ def test_what_lies_outside_does_not_matter():
     assert (dk8.cpu()[untouched] == 0).all() and (dv8.cpu()[untouched] == 0).all()
 
 
+@pytest.mark.parametrize("h_q,h_kv,d,rows,window,sinks", [
+    (8, 2, 128, 1, 100, 4), (8, 2, 64, 1, 1, 0), (16, 2, 128, 1, 700, 70), (3, 3, 64, 1, 65, 0),
+    (4, 1, 128, 20, 90, 3), (2, 1, 64, 61, 64, 130), (4, 4, 128, 128, 1, 1)])
+def test_keys_given_up(h_q, h_kv, d, rows, window, sinks):
+    """The newest rows of cached sequences whose keys between the sinks and the window of the
+    first of those rows are NaN or infinite, as are those past the last row.  At most 128 rows
+    times heads of a KV group, so that a tile's rows are one work item."""
+    held, room = [rows, 129, 1000, 1337, 650], [rows + 3, 200, 1000, 1500, 651]
+    say(f"[keys given up] heads=({h_q},{h_kv}) d={d} rows={rows} window={window} sinks={sinks}")
+    starts = np.cumsum([0] + room[:-1])
+    tiles = tile_list([(int(s) + n - rows, int(s) + n, 0, h_q) for s, n in zip(starts, held)])
+    n_q, n_kv = rows * len(held), sum(room)
+    q, k, v, _ = tensors(rows + window, n_q, n_kv, h_q, h_kv, d)
+    ok = ref.visible(room, ref.positions(tiles), n_kv, window, sinks)
+    want = ref.attention(q, k, v, ok, ref.coverage(tiles, n_q, h_q))
+    junk = ~ok.any(0)
+    assert junk.sum() > 100
+    k[junk], v[junk] = torch.nan, torch.inf
+    o, lse = pl.libra_attn_window_fwd(*dev(q, k, v), offsets(room),
+                                      pl.tiles_to_device(tiles, DEV), window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    ref.close("o", o, want["o"])
+    ref.close("lse", lse, want["lse"])
+
+
 def _step(q, k, v, do, cu, td, mask, bufs):
     """Forward, checkpoint and both backwards into `bufs`, as one layer runs them."""
     o, lse, dq, dk, dv, ws, held, dq8, dk8, dv8 = bufs
