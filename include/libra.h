@@ -445,8 +445,9 @@ int libra_attn_bwd(const void *q, const void *k, const void *v, const void *o, c
  * Inputs: k and v must be finite from a sample's first key to the last row
  * that the tiles cover in it, and q, o, lse and dout in the covered
  * (row, head) pairs; nothing else is used.
- * Split K: a call with fewer than two work items per workgroup cuts items of
- * 8 or more 64-key blocks into key ranges as libra_attn_fwd does.  dK / dV of
+ * Split K: a call of few work items whose rows can reach 24 64-key blocks cuts
+ * the longer ones into key ranges as libra_attn_fwd does; so does a call of
+ * single tokens, with 4 blocks or more.  dK / dV of
  * sink keys are summed over parts of a long sample's rows, in row order.
  * Results are the same from one call to the next.
  */

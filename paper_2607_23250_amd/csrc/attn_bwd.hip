@@ -1398,10 +1398,12 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
                        static_cast<uint4 *>(dv), n16, (unsigned)(T * kTileSplit), kv_blocks,
                        2 * zero_blocks, win, q8, 1};
     if constexpr (WIN) {
-      // Eight workgroups per CU in all: each looks at the maxima found so far, one address
-      // for all of them (68 tiles of a 20K pack: 44 us with 64 for each tile, 31 with 15; the
-      // 32 tiles of a 32K pack: 155 us with 64, 171 with 32).
-      pass.tile_split = (unsigned)std::max<int64_t>(1, std::min<int64_t>(kTileSplit, 8 * cus / T));
+      // Workgroups for 64 KB of Q and dO or more, at most eight per CU in all: each looks at
+      // the maxima found so far, one address for all of them (whole backward of a 20K pack, 12
+      // heads of 64, 61 MB: 338 us with 32 KB for each, 325 with 64; the pass over a 32K pack of
+      // 32 heads of 128, 537 MB: 155 us with eight per CU, 171 with four).
+      const int64_t groups = std::min<int64_t>(8 * cus, n_q * h_q * D * 4 / 65536 + 1);
+      pass.tile_split = (unsigned)std::max<int64_t>(1, std::min<int64_t>(kTileSplit, groups / T));
       pass.tile_blocks = (unsigned)T * pass.tile_split;
     }
     hipLaunchKernelGGL(HIP_KERNEL_NAME(bwd_max_kernel<D, WIN, HELD>),

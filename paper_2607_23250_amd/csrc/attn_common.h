@@ -204,9 +204,12 @@ __device__ __forceinline__ int take_item(int32_t *hdr, int base, int q, int &sta
 }
 
 // Items of about equal cost (windowed attention) stay in one list of hdr[base +
-// kXcds] entries (at most hdr[base + 2 kXcds]) instead of a sorted segment per queue: runs of 2^shift
-// neighbours, which read the same K / V rows or query blocks, go to the XCDs in
-// turn.  Queue x holds the items of its runs, in list order.
+// kXcds] entries (at most hdr[base + 2 kXcds]) instead of a sorted segment per
+// queue: runs of 2^shift neighbours, which read the same K / V rows or query
+// blocks, go to the XCDs in turn.  Queue x holds the items of its runs, in list order.  (Forward of a 32K
+// pack, window 1024: 659 us with single items, 632 with runs of 8, 615 with 64;
+// runs of 64 leave CUs idle in short lists: backward of 65536 tokens, 2 KV heads,
+// 1060 dK / dV items, 1152 us, 1124 with 8.)
 __host__ __device__ constexpr int run_shift(int n) { return n >= 4096 ? 6 : n >= 512 ? 3 : 0; }
 __device__ __forceinline__ int run_count(int n, int sh, int x) {
   const int rest = (n & ((kXcds << sh) - 1)) - (x << sh);
@@ -270,7 +273,9 @@ __device__ __forceinline__ bf16x8 held8(const Held &x, size_t at) {
 // A sample whose rows reach this far past the window of its first key has the
 // gradients of its sink keys summed over those far rows by a kernel of their
 // own; in shorter ones the far rows are part of the sink keys' dK / dV items.
-constexpr int kFarRows = 512;
+// (Backward of 4096 tokens, 8 / 2 heads, window 256, 4 sinks: 196 us with 512, 157 with 256 and
+// 128; of 8192, 32 / 4 heads, window 512: 794 with 2048, 474, 449, 446.)
+constexpr int kFarRows = 256;
 __host__ __device__ __forceinline__ bool far_sample(const Window &w, int64_t len) {
   return w.sinks > 0 && len > (int64_t)w.size + kFarRows;
 }

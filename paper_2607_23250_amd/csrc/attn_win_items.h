@@ -40,9 +40,16 @@ struct WinPrep {
   int max_parts;   // 0: no item is split
   FwdSplit *splits;
 };
-constexpr int kWinMinSteps = 4;   // a part of a split item walks at least 4 key blocks
+// A part of a split item walks at least 6 key blocks (backward of 4096 tokens, 2 / 1 heads,
+// window 4096: 142 us with 4, 132 with 6, 134 with 8; forward of 2000: 34, 38, 42).
+constexpr int kWinMinSteps = 6;
+// Items of fewer steps than these are not split: the parts' merge takes longer than it saves
+// (forward of 4096 tokens, 8 / 2 heads, d = 64, window 1024, 21 steps: 46 us split, 36 whole;
+// of 2000 tokens, 2 / 1 heads, 34 steps: 38 split, 43 whole).
+constexpr int kWinSplitSteps = 24;
 // Calls of at most this many (row, query head) pairs have one workgroup build their
-// items; it clears the header itself and can split items.
+// items; it clears the header itself (16K tokens, window 128 to 256: 8 heads 38 us with one
+// workgroup and 39 with many, 32 heads 157 and 140).
 constexpr int64_t kWinAlonePairs = 131072;
 
 struct WinTile {   // of a tile, what its items need
@@ -173,7 +180,11 @@ struct WinRows {
   int cuts;     // key ranges of a single row's item at most
   int64_t units() const { return T * chunks * parts; }
 };
-constexpr int kRowMinSteps = 2;   // a key range of a single row walks at least 2 key blocks
+// A key range of a single row walks at least 2 key blocks (one sequence, 17 blocks: 13.1 us,
+// 14.6 with at least 4), and an item has at most 64 of them (20000 keys, one chunk of 4 heads:
+// 22.7 us with up to 32, 18.9 with 64, 19.4 with 256).
+constexpr int kRowMinSteps = 2;
+constexpr int kRowMaxCuts = 64;
 // Key ranges of a single row's item of this many steps.
 __device__ __forceinline__ int row_parts(int steps, int cuts) {
   return max(1, min(cuts, steps / kRowMinSteps));
@@ -276,7 +287,8 @@ __device__ __forceinline__ void clear_win_header(int32_t *hdr, int grid_q, int64
 // rows) or many, each with an equal run of the units (tile, head chunk, 32-row window).
 //
 // Split K: a call with fewer items than twice `split_grid` cuts items of at least two parts
-// into key ranges of about a quarter of a workgroup's share, as the causal calls do; one
+// into key ranges of about half a workgroup's share (forward of 12000 tokens, 4 / 2 heads, no
+// key outside the window: 268 us with a whole share, 178 with half, 182 with a quarter); one
 // workgroup then builds the list, and the parts' slots go by its order, so that nothing
 // depends on which part runs where.
 __device__ __forceinline__ void prep_win(const WinPrep &a, WinPrepLds &lds, unsigned block,
@@ -401,7 +413,7 @@ __device__ __forceinline__ void prep_win(const WinPrep &a, WinPrepLds &lds, unsi
     const unsigned long long items = lds.items, work = lds.work, gr = (unsigned)a.split_grid;
     if (items > 0 && items < 2 * gr) {
       // items longer than C number at most work / C, their parts at most twice that
-      const unsigned long long c = (work + 4 * gr - 1) / (4 * gr);
+      const unsigned long long c = (work + 2 * gr - 1) / (2 * gr);
       const unsigned long long fit = (2 * work + a.max_parts - 1) / (unsigned)a.max_parts;
       const unsigned long long m = c > fit ? c : fit;
       chunk = (int)(m > kWinMinSteps ? m : kWinMinSteps);
@@ -489,7 +501,9 @@ struct WinSink {
   int32_t base, parts;
 };
 constexpr int kMaxSinks = 1024;
-constexpr int kSinkPartRows = 128;   // rows of a part of far rows at least
+// Rows of a part of far rows at least (backward of 8192 tokens, 32 / 4 heads, window 512,
+// 4 sinks: 500 us with 512, 465 with 128 and with 32).
+constexpr int kSinkPartRows = 128;
 constexpr int kSinkParts = 256;      // slots beyond one for each WinSink
 __host__ __device__ constexpr int sink_blocks(const Window &w) { return (w.sinks + 31) / 32; }
 __host__ __device__ constexpr size_t sink_part_floats(int d) { return (size_t)2 * 32 * d; }
@@ -524,7 +538,8 @@ struct WinBwdPrep {
   int parts;
 };
 // Row ranges of a dK / dV item.  A call of few key blocks and KV heads (4K tokens and 2 KV
-// heads: 66 items for 256 CUs) cuts each into as many as the CUs hold, of at least 8 row blocks.
+// heads: 66 items for 256 CUs) cuts each into as many as the CUs hold, of at least 8 row blocks,
+// and up to 8 (2 / 1 heads, window 4096: 145 us; 163 with up to 4; no less with 16).
 inline int win_kv_parts(const Window &w, int64_t key_blocks, int h_kv, int cus) {
   const int64_t fit = cus / (key_blocks * h_kv);
   const int64_t most = ((int64_t)w.size + kBwdBK) / (kBwdSplitMinBlocks * kRows);
@@ -533,18 +548,20 @@ inline int win_kv_parts(const Window &w, int64_t key_blocks, int h_kv, int cus) 
 }
 constexpr int kWinMaxSplits = 512;   // split dK / dV items of a call (more than CUs / 2)
 
-// Steps of an item at most: its rows' window, the rows (at most 128) and the sinks.
-inline int64_t win_max_steps(const Window &w, int64_t n_kv) {
-  const int64_t reach = (int64_t)w.size + kFwdPartRows + kFwdBN;
+// Steps of an item of up to `rows` rows at most: their window, the rows and the sinks.
+inline int64_t win_max_steps(const Window &w, int64_t n_kv, int rows = kFwdPartRows) {
+  const int64_t reach = (int64_t)w.size + rows + kFwdBN;
   return (reach < n_kv ? reach : n_kv) / kFwdBN + 1 + (w.sinks + kFwdBN - 1) / kFwdBN;
 }
-// Can a call split an item?  One of two parts or more.
+// Can a call split an item?  Shorter ones take less time than their parts' merge.
 inline bool win_may_split(const Window &w, int64_t n_kv) {
-  return win_max_steps(w, n_kv) >= 2 * kWinMinSteps;
+  return win_max_steps(w, n_kv) >= kWinSplitSteps;
 }
 // Single tokens beyond this many (tile, head chunk) pairs go through the list.
 constexpr int64_t kMaxRowJobs = 1 << 20;
-// Other calls without a list have at most this many units.
+// Other calls without a list have at most this many units (8 / 2 heads, d = 64, window 128:
+// 4096 tokens in tiles of 512, 2048 units: 19.9 us, 22.9 with a list; 16384 tokens in tiles of
+// 2048, 8192 units, most of them past their tile's end: 55, 39 with a list).
 constexpr int64_t kMaxSmallUnits = 4096;
 
 // Arguments of the windowed dQ kernel (attn_window_dq.hip).  q and o, or q8 and o8.

@@ -374,21 +374,23 @@ win_fwd_kernel(WinFwd a, R rows) {
 }
 
 // Merges the parts of single tokens: a workgroup to a (tile, head chunk), whose item it finds
-// as the attention kernel does; the recurrence of fwd_combine_kernel, eight columns to a
-// thread.
+// as the attention kernel does.  Eight columns to a thread; the threads beyond 4 heads x D / 8
+// share the parts (`p` mod `kGroups`), each with the recurrence of fwd_combine_kernel, and the
+// groups' sums are merged in the same way.
 template <int D>
 __global__ __launch_bounds__(256) void win_rows_combine_kernel(WinRows a,
                                                                const float *__restrict__ parts,
                                                                bf16 *__restrict__ o,
                                                                float *__restrict__ lse) {
   constexpr size_t PF = fwd_part_floats(D);
-  constexpr int C = D / 8;   // threads of a row
+  constexpr int C = D / 8, kSlots = 4 * C, kGroups = 256 / kSlots;
+  __shared__ float s_acc[kGroups][8][kSlots], s_m[kGroups][kSlots], s_l[kGroups][kSlots];
   RowUnit unit(a, (int64_t)blockIdx.x * a.parts);
   FwdItem it;
   if (!unit.valid || !unit.one_row() || !unit.next(a, it) || it.slot < 0) return;
   // the first part of np: all but the last are as long
-  const int head_i = threadIdx.x / C, col = threadIdx.x % C * 8;
-  if (head_i >= it.nh) return;
+  const int slot = threadIdx.x % kSlots, group = threadIdx.x / kSlots;
+  const int head_i = min(slot / C, it.nh - 1), col = slot % C * 8;
   const WinTile &t = unit.t;
   const FwdItem whole = win_item(t, it.sample, t.q_begin, t.q_end, 0, 1, it.g, it.head0, it.nh,
                                  a.win);
@@ -397,15 +399,15 @@ __global__ __launch_bounds__(256) void win_rows_combine_kernel(WinRows a,
   const int pr = head_i * kRows;   // wave slice head_i, its first row
   float m = -INFINITY;
 #pragma unroll 4
-  for (int p = 0; p < np; ++p) m = fmaxf(m, rec[p * PF + (size_t)kFwdPartRows * D + pr]);
+  for (int p = group; p < np; p += kGroups)
+    m = fmaxf(m, rec[p * PF + (size_t)kFwdPartRows * D + pr]);
   float l = 0.f, acc[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) acc[i] = 0.f;
 #pragma unroll 4
-  for (int p = 0; p < np; ++p) {
+  for (int p = group; p < np; p += kGroups) {
     const float *pt = rec + p * PF;
-    const float mp = pt[(size_t)kFwdPartRows * D + pr];
-    const float wgt = mp == -INFINITY ? 0.f : fast_exp2(mp - m);
+    const float wgt = fast_exp2(pt[(size_t)kFwdPartRows * D + pr] - m);   // finite, both
     l += wgt * pt[(size_t)kFwdPartRows * D + kFwdPartRows + pr];
     const float4 *src = reinterpret_cast<const float4 *>(pt + (size_t)pr * D + col);
 #pragma unroll
@@ -416,6 +418,24 @@ __global__ __launch_bounds__(256) void win_rows_combine_kernel(WinRows a,
       acc[4 * i + 2] += wgt * x.z;
       acc[4 * i + 3] += wgt * x.w;
     }
+  }
+  s_m[group][slot] = m;
+  s_l[group][slot] = l;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s_acc[group][i][slot] = acc[i];
+  __syncthreads();
+  if (group > 0 || slot / C >= it.nh) return;
+#pragma unroll
+  for (int u = 1; u < kGroups; ++u) m = fmaxf(m, s_m[u][slot]);
+  l = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+#pragma unroll
+  for (int u = 0; u < kGroups; ++u) {
+    const float wgt = fast_exp2(s_m[u][slot] - m);   // 0 for a group without parts
+    l += wgt * s_l[u][slot];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] += wgt * s_acc[u][i][slot];
   }
   const float inv = 1.f / l;
   const int head = it.head0 + head_i;
@@ -428,18 +448,20 @@ __global__ __launch_bounds__(256) void win_rows_combine_kernel(WinRows a,
 }
 
 // How a call without a list runs (parts, cuts); false: it has one.
-//   * Single tokens, no more Q rows than tiles: up to eight units for each CU, one for each key
-//     range, as long as the slots of their partial results suffice.
+//   * Single tokens, no more Q rows than tiles: one unit for each key range, as many as run at
+//     once, two for each CU, and have slots for their partial results (32 / 8 heads, window
+//     4096: 32 sequences of 6000 keys 121 us with one for each CU, 98 with two, 105 with four;
+//     64 sequences 181, 181 and 191).
 //   * Small calls whose items are too short to be cut: as many units as the longest tile that
 //     the rows allow has windows, so that none has two (512 tokens, 8 / 2 heads, window 128:
 //     16.6 us with a list, 9.9 without).
 static bool without_list(WinRows &r, int max_parts, int cus) {
   const int64_t jobs = r.T * r.chunks;
-  const int64_t steps = win_max_steps(r.win, r.n_kv);
   if (r.n_q <= r.T && jobs <= kMaxRowJobs) {
-    const int64_t most = std::min<int64_t>(steps / kRowMinSteps, max_parts / jobs);
-    r.cuts = r.parts =
-        (int)std::max<int64_t>(1, std::min<int64_t>(most, 8 * (int64_t)cus / jobs));
+    const int64_t steps = win_max_steps(r.win, r.n_kv, 1);
+    const int64_t most = std::min<int64_t>(std::min<int64_t>(steps / kRowMinSteps, kRowMaxCuts),
+                                           std::min<int64_t>(max_parts, 2 * cus) / jobs);
+    r.cuts = r.parts = (int)std::max<int64_t>(most, 1);
     return true;
   }
   const int64_t windows = (r.n_q + kRows - 1) / kRows;
