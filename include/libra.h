@@ -312,143 +312,10 @@ int libra_attn_bwd(const void *q, const void *k, const void *v, const void *o, c
  * sinks and the window of its first row (they may have been given up).
  * Backward: k and v must be finite from a sample's first key to the last row
  * that the tiles cover in it.  Nothing else is used.
- * Split K: a call with fewer than two work items per workgroup (few rows and
- * heads against long samples) cuts its long items into key ranges that run in
- * parallel and merges their partial results (the online-softmax recurrence
- * across ranges); the result is the same up to the order of fp32 additions.
- * Rows and heads are processed independently of how tiles group them, so the
- * output does not depend on B, H or the worker a tile was placed on; it is
- * bit-identical across such groupings whenever no item is split.
- */
-int libra_attn_fwd(const void *q, const void *k, const void *v, const int64_t *cu_seqlens,
-                   int64_t num_samples, const libra_tile_t *tiles, int64_t num_tiles,
-                   int64_t n_q_rows, int64_t n_kv_rows, int32_t h_q, int32_t h_kv,
-                   int32_t head_dim, float softmax_scale, void *o, float *lse, void *workspace,
-                   size_t workspace_bytes, void *stream);
-
-/*
- * Tiles that do not lie inside the buffers a call describes (q_begin < 0,
- * q_end > n_kv_rows, empty ranges, rows past n_q_rows, heads outside
- * [0, h_q)) are skipped on the device: the call still returns LIBRA_OK and
- * computes every other tile exactly as without them.  The number skipped by
- * the last libra_attn_fwd or libra_attn_bwd call that used a workspace is an
- * int32 at byte offset LIBRA_WS_SKIPPED_OFFSET of that workspace (plus 1 if
- * the workspace's work-item list overflowed, which a workspace of
- * libra_attn_workspace_size bytes rules out).
- *
- * libra_attn_skipped_tiles -- copies that count to *count after the work
- * already enqueued on `stream` has finished (it synchronizes `stream`).
- *   workspace: the device workspace of that call (256-byte aligned).
- * Errors: EINVAL (NULL arguments), EHIP.
- *
- * Tiles that overlap in (row, head) are not detected.  Each copy is computed
- * in full: O, LSE and dQ of the shared pairs are written twice with the same
- * values, and dK / dV receive their contribution twice.  libra_plan never
- * produces overlapping tiles.
- */
-#define LIBRA_WS_SKIPPED_OFFSET 16
-int libra_attn_skipped_tiles(const void *workspace, int32_t *count, void *stream);
-
-/*
- * libra_attn_fwd_noalloc -- libra_attn_fwd without a workspace argument, for
- * callers that cannot allocate device memory (code under HIP graph capture,
- * tight serving loops, harnesses that forbid allocation).  Same arguments,
- * semantics and errors as libra_attn_fwd, with the same kernels but without
- * split K (its partial slots would not fit), so its results equal
- * libra_attn_fwd's whenever that call splits no item; the work items live in
- * a device array built into the library, of LIBRA_FWD_NOALLOC_MAX_WORKSPACE
- * bytes and a small header, one per device, held until the process ends.  The call allocates
- * nothing and frees nothing (its first call on a device looks up that
- * device's array).
- *   Sizes whose work-item list (48 bytes per item, bounded from the sizes as
- *   for libra_attn_workspace_size) exceeds the array are rejected with
- *   LIBRA_ENOSPC before anything is enqueued (16 MiB covers, e.g., 65536
- *   query rows x 32 heads of a 1M-token pack).
- *   Every call on one device shares that device's array: calls that overlap
- *   in time on one device (different streams, or host threads) race and
- *   must be serialized by the caller.  Each call's preparation pass rewrites
- *   every part of the array it later reads, so nothing needs clearing
- *   between calls.  The skipped-tile count of these calls is not exposed.
- */
-#define LIBRA_FWD_NOALLOC_MAX_WORKSPACE ((size_t)16 << 20)
-int libra_attn_fwd_noalloc(const void *q, const void *k, const void *v,
-                           const int64_t *cu_seqlens, int64_t num_samples,
-                           const libra_tile_t *tiles, int64_t num_tiles, int64_t n_q_rows,
-                           int64_t n_kv_rows, int32_t h_q, int32_t h_kv, int32_t head_dim,
-                           float softmax_scale, void *o, float *lse, void *stream);
-
-/* libra_attn_bwd flags */
-#define LIBRA_BWD_ACCUMULATE_DKV 1u /* dk, dv are fp32 and are added to (not overwritten) */
-
-/*
- * libra_attn_bwd -- gradients of sum(dO * O) for the rows and heads covered
- * by the tiles (the textbook attention backward; the paper's backward reuses
- * the forward assignment, Sec. 4.3.3):
- *     P = exp(q K^T * scale - LSE),  D = rowsum(dO * O),
- *     dV = P^T dO,  dS = P * (dO V^T - D),  dQ = scale * dS K,  dK = scale * dS^T q,
- * with dK / dV summed over the query heads of each KV head.
- *   q, k, v, o, dout: bf16 device tensors as in libra_attn_fwd; lse fp32 as
- *       returned by libra_attn_fwd for the same tiles.
- *   dq [n_q_rows][h_q][d] bf16: covered (row, head) entries are written.
- *   dk, dv [n_kv_rows][h_kv][d]: bf16, every element written (zero where no
- *       covered row attends); with LIBRA_BWD_ACCUMULATE_DKV they are fp32 and
- *       this call's contribution is added, so several disjoint tile sets
- *       (virtual workers) can be summed into one caller-zeroed buffer.
- *   workspace: >= libra_attn_workspace_size(..., 1) bytes, 256-byte aligned.
- * Precision: the dK / dV products take fp16 copies of q, dout, k and v, each
- * scaled by a power of two from its max |x| over what the products read, so
- * that P and dS round to 11 significant bits instead of bf16's 8; the scales
- * are undone exactly on output.  dQ's products take the bf16 inputs.
- * Inputs: every element of k and v in the samples the tiles touch, and of
- * q, dout, o and lse in the covered (row, head) pairs, must be finite.
- * Other rows of q, dout, o and lse are not read by the dK / dV products
- * (their fp16 copies hold zeros there).
- * Split K: the dQ products split their work items into key ranges as the
- * forward does, when the call's items would leave more than a tenth of the
- * workgroups idle; the parts' fp32 dQ and sums of dS are merged before the
- * dK / dV products read D.  The workspace holds those partial results too.
- * Split rows: the dK / dV products cut their work items (128 keys of a KV head
- * against all rows that attend them) into row ranges when the longest item
- * would take a quarter longer than an even spread of the call's work (few
- * samples and KV heads), counting the rows that the tiles cover.  Their fp32
- * partial sums are added in row order, so the result is the same up to the
- * order of fp32 additions, and the same from one call to the next.
- */
-int libra_attn_bwd(const void *q, const void *k, const void *v, const void *o, const float *lse,
-                   const void *dout, const int64_t *cu_seqlens, int64_t num_samples,
-                   const libra_tile_t *tiles, int64_t num_tiles, int64_t n_q_rows,
-                   int64_t n_kv_rows, int32_t h_q, int32_t h_kv, int32_t head_dim,
-                   float softmax_scale, void *dq, void *dk, void *dv, uint32_t flags,
-                   void *workspace, size_t workspace_bytes, void *stream);
-
-/*
- * Windowed attention: libra_attn_fwd and libra_attn_bwd with a sliding window
- * and sinks.  The row at sample-local position p attends, of its own sample,
- * the keys
- *     { k <= p : k > p - window or k < sinks },
- * its own key, the window - 1 before it and the sample's first `sinks` keys.
- * O, LSE, dQ, dK and dV are those of libra_attn_fwd / libra_attn_bwd under
- * this mask.  A row always attends its own key, so no row is empty; a window
- * of at least the longest sample gives causal attention.
- *   window >= 1; 0 <= sinks <= 1024 (EUNSUPPORTED above).  Values past
- *       n_kv_rows act as n_kv_rows.  The backward takes those of the forward.
- *   All other arguments, layouts, flags, errors, the handling of tiles that
- *       are out of range and the timing records: as in libra_attn_fwd and
- *       libra_attn_bwd.
- *   workspace: >= libra_attn_window_workspace_size bytes for the same window,
- *       sinks and direction, 256-byte aligned (0 bytes: invalid sizes).
- * Single tokens: a tile may be one row.  For a batch of cached sequences,
- * cu_seqlens holds the sequences' places in k and v, and each has one tile of
- * its newest position.  A sequence's place may be longer than what it holds:
- * keys past a tile's last row (of the forward's work item, at most 128 rows)
- * are not read.
- * Inputs: k and v must be finite from a sample's first key to the last row
- * that the tiles cover in it, and q, o, lse and dout in the covered
- * (row, head) pairs; nothing else is used.
  * Split K: a call of few work items whose rows can reach 24 64-key blocks cuts
  * the longer ones into key ranges as libra_attn_fwd does; so does a call of
- * single tokens, with 4 blocks or more.  dK / dV of
- * sink keys are summed over parts of a long sample's rows, in row order.
+ * single tokens, with 4 blocks or more.  dK / dV of sink keys are summed over
+ * parts of a long sample's rows, in row order.
  * Results are the same from one call to the next.
  */
 size_t libra_attn_window_workspace_size(int64_t num_tiles, int64_t num_samples, int64_t n_q_rows,
@@ -530,11 +397,11 @@ int libra_attn_bwd_ckpt8(const libra_ckpt8_t *q, const libra_ckpt8_t *k, const l
  * Kernel timing (tracing aid).  libra_timing_enable(1) clears the records of
  * the calling thread and makes every later libra_attn_fwd / libra_attn_bwd
  * call (windowed and checkpoint ones too) on that thread record HIP events on
- * its stream around its main
- * persistent kernels (the work-item kernels, not the small preparation
- * passes); libra_timing_enable(0) stops recording.  libra_timing_read waits
- * for the recorded events and returns the summed milliseconds and the number
- * of launches since the last enable of: which = 0, the forward kernel;
+ * its stream around its main persistent kernels (the work-item kernels, not
+ * the small preparation passes); libra_timing_enable(0) stops recording.
+ * libra_timing_read waits for the recorded events and returns the summed
+ * milliseconds and the number of launches since the last enable of: which =
+ * 0, the forward kernel;
  * 1, the backward dK/dV kernel; 2, the backward dQ kernel.
  * Errors: EINVAL (bad `which`, NULL outputs), EHIP.
  */
