@@ -65,6 +65,9 @@ def _cases():
     # a context-parallel share: rows at both ends of a long sample
     yield "share", [2000], blocks(2000, 128, 4, 2, [(0, 200), (1800, 2000)]), (4, 2), 128, 150, 4
     yield "deep_tile", [30, 2500], tile_list([(2300, 2420, 0, 2)]), (4, 2), 64, 300, 33
+    # items long enough to be cut into key ranges
+    yield "cut", [2600, 40], blocks(2640, 300, 4, 2), (4, 2), 128, 2500, 3
+    yield "cut_3_heads", [7, 1900], blocks(1907, 512, 3), (3, 1), 64, 1800, 0
     # rows past the last sample
     yield "past_the_end", [100, 150], blocks(320, 64, 2), (2, 2), 64, 30, 2
 
@@ -137,6 +140,25 @@ def test_single_tokens(h_q, h_kv, d, window, sinks):
         empty[int(s):int(s) + n] = False
     k[empty], v[empty] = torch.nan, torch.nan
     o, lse = pl.libra_attn_window_fwd(*dev(q, k, v), offsets(room),
+                                      pl.tiles_to_device(tiles, DEV), window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    ref.close("o", o, want["o"])
+    ref.close("lse", lse, want["lse"])
+
+
+@pytest.mark.parametrize("h_q,h_kv,d,window", [(4, 1, 64, 20000), (8, 2, 128, 9000),
+                                               (2, 1, 128, 17001), (5, 1, 64, 2000)])
+def test_single_tokens_of_long_caches(h_q, h_kv, d, window):
+    """Two sequences whose keys are cut into many ranges, and one of two key blocks."""
+    held, sinks = [17000, 70, 9990], 5
+    say(f"[long caches] heads=({h_q},{h_kv}) d={d} window={window}")
+    ends = np.cumsum(held)
+    tiles = tile_list([(int(e) - 1, int(e), 0, h_q) for e in ends])
+    n_kv = int(ends[-1])
+    q, k, v, _ = tensors(d + window, len(held), n_kv, h_q, h_kv, d)
+    ok = ref.visible(held, ref.positions(tiles), n_kv, window, sinks)
+    want = ref.attention(q, k, v, ok, ref.coverage(tiles, len(held), h_q))
+    o, lse = pl.libra_attn_window_fwd(*dev(q, k, v), offsets(held),
                                       pl.tiles_to_device(tiles, DEV), window=window, sinks=sinks)
     torch.cuda.synchronize()
     ref.close("o", o, want["o"])
