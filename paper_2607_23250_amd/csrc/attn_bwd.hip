@@ -506,7 +506,7 @@ __device__ __forceinline__ void absmax_q(unsigned block, unsigned split,
     const int64_t row = m * kRows + r;
     const bool ok = row >= ra && row < rb && !(WIN && row >= past);
     if constexpr (WIN) {
-      // bound by memory: 805 MB of Q, dO, K and V and of zeroed gradients in 155 us
+      // bound by memory: 671 MB of Q, dO, K and V in 125 us
       if (ok) {
         for (int h = tl.head_begin; h < tl.head_end; ++h) {
           const size_t off = ((size_t)row * h_q + h) * D + part * (D / 8);
@@ -549,14 +549,19 @@ __device__ __forceinline__ void absmax_q(unsigned block, unsigned split,
 // (all KV heads).  One wave per key row.  CONVERT = false: max |K| and
 // max |V| over them; CONVERT = true: their scaled fp16 copies.
 // WIN: `ext` holds WinSample records; keys that no covered row's window or sinks
-// reach, and keys past the last covered row, are left out.
+// reach, and keys past the last covered row, are left out; and (CONVERT = false, dk not
+// null) dK and dV become zero where no dK / dV item will write them: zeroing all of both
+// (134 MB on a 32K pack) took 27 us.
 template <int D, bool CONVERT, bool WIN>
 __device__ __forceinline__ void kv_pass(unsigned block, unsigned blocks,
                                         const bf16 *__restrict__ k, const bf16 *__restrict__ v,
                                         const int64_t *__restrict__ cu, int64_t n,
                                         const int32_t *__restrict__ ext, int h_kv, int64_t n_kv,
                                         int32_t *__restrict__ hdr, f16 *__restrict__ k16,
-                                        f16 *__restrict__ v16, const Window &win) {
+                                        f16 *__restrict__ v16, const Window &win,
+                                        const WinBlock *__restrict__ blocks_of = nullptr,
+                                        uint4 *__restrict__ dk = nullptr,
+                                        uint4 *__restrict__ dv = nullptr) {
   const int l = threadIdx.x & 63;
   const int64_t wave = ((int64_t)block * 256 + threadIdx.x) >> 6;
   const int64_t waves = (int64_t)blocks * 4;
@@ -568,6 +573,7 @@ __device__ __forceinline__ void kv_pass(unsigned block, unsigned blocks,
   }
   int64_t lo = 0, hi = 0, end = 0;   // rows [lo, hi) of the current sample; loaded keys end at `end`
   int64_t from = 0, sink_end = 0;    // WIN: and start at `from`, but for those before sink_end
+  int64_t place = 0;                 // WIN: of the sample's key block 0
   for (int64_t row = wave; row < n_kv; row += waves) {
     if (row < lo || row >= hi) {
       const int64_t j = upper_bound64(cu, n, row) - 1;
@@ -576,12 +582,24 @@ __device__ __forceinline__ void kv_pass(unsigned block, unsigned blocks,
       if constexpr (WIN) {
         const WinSample &ws = reinterpret_cast<const WinSample *>(ext)[j];
         end = lo + ws.ext;
+        place = block_place(lo, j);
         from = lo + first_key_block(ws.beg, win) * kBwdBK;
         sink_end = lo + (win.sinks + kBwdBK - 1) / kBwdBK * kBwdBK;
       } else {
         const int64_t e = (int64_t)ext[j];
         const int64_t lim = (e + kBwdBK - 1) / kBwdBK * kBwdBK;
         end = lo + (e > 0 ? (lim < hi - lo ? lim : hi - lo) : 0);
+      }
+    }
+    if constexpr (WIN && !CONVERT) {
+      if (dk) {
+        const unsigned long long mask =
+            row < end ? blocks_of[place + (row - lo) / kBwdBK].mask : 0;
+        for (int c = l; c < chunks; c += 64)
+          if (!(mask >> (c / (D / 8)) & 1ull)) {
+            dk[row * chunks + c] = make_uint4(0, 0, 0, 0);
+            dv[row * chunks + c] = make_uint4(0, 0, 0, 0);
+          }
       }
     }
     if (row >= end) continue;
@@ -716,6 +734,7 @@ struct BwdPass {
   Window win;
   Held q8;
   unsigned tile_split;   // windowed: workgroups of a tile in the max pass
+  const WinBlock *blocks;
 };
 template <int D, bool WIN, bool HELD>
 __global__ __launch_bounds__(256) void bwd_max_kernel(BwdPass a) {
@@ -723,7 +742,7 @@ __global__ __launch_bounds__(256) void bwd_max_kernel(BwdPass a) {
   if (b == 0 && threadIdx.x == 0 && a.hdr[kDqFull]) atomicAdd(&a.hdr[kBadTiles], 1);
   if (b < a.kv_blocks) {
     kv_pass<D, false, WIN>(b, a.kv_blocks, a.k, a.v, a.cu, a.n, a.ext, a.h_kv, a.n_kv, a.hdr,
-                           a.k16, a.v16, a.win);
+                           a.k16, a.v16, a.win, a.blocks, WIN && a.n16 ? a.dk : nullptr, a.dv);
   } else if ((b -= a.kv_blocks) < a.tile_blocks) {
     absmax_q<D, WIN, HELD>(b, WIN ? a.tile_split : kTileSplit, a.q, a.q8, a.dout, a.tiles, a.h_q,
                            a.n_q, a.n_kv, a.cu[a.n], a.hdr, a.rec);
@@ -1394,17 +1413,19 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
     const unsigned kv_blocks =
         (unsigned)std::max<int64_t>(1, std::min<int64_t>((n_kv + 31) / 32, (int64_t)cus * 8));
     BwdPass pass{q, k, v, o, dout, lse, cu, n, tiles, h_q, h_kv, n_q, n_kv, L.nq_pad, scale,
-                       hdr, ext, rec, k16, v16, stats, static_cast<uint4 *>(dk),
-                       static_cast<uint4 *>(dv), n16, (unsigned)(T * kTileSplit), kv_blocks,
-                       2 * zero_blocks, win, q8, 1};
+                 hdr, ext, rec, k16, v16, stats, static_cast<uint4 *>(dk),
+                 static_cast<uint4 *>(dv), n16, (unsigned)(T * kTileSplit), kv_blocks,
+                 2 * zero_blocks, win, q8, 1, nullptr};
     if constexpr (WIN) {
       // Workgroups for 64 KB of Q and dO or more, at most eight per CU in all: each looks at
       // the maxima found so far, one address for all of them (whole backward of a 20K pack, 12
       // heads of 64, 61 MB: 338 us with 32 KB for each, 325 with 64; the pass over a 32K pack of
-      // 32 heads of 128, 537 MB: 155 us with eight per CU, 171 with four).
+      // 32 heads of 128, 537 MB, with zeroed gradients: 155 us with eight per CU, 171 with four).
       const int64_t groups = std::min<int64_t>(8 * cus, n_q * h_q * D * 4 / 65536 + 1);
       pass.tile_split = (unsigned)std::max<int64_t>(1, std::min<int64_t>(kTileSplit, groups / T));
       pass.tile_blocks = (unsigned)T * pass.tile_split;
+      pass.blocks = reinterpret_cast<const WinBlock *>(ws + L.gmask);
+      pass.zero_blocks = 0;
     }
     hipLaunchKernelGGL(HIP_KERNEL_NAME(bwd_max_kernel<D, WIN, HELD>),
                        dim3(pass.kv_blocks + pass.tile_blocks + pass.zero_blocks), dim3(256), 0,
