@@ -2,12 +2,17 @@
 //
 // Its mathematics is the causal dQ kernel's (attn_bwd_dq.hip): S^T = K Q^T, dP^T - D =
 // [V | 1] [dO | -D]^T, dS^T = P^T (dP^T - D), dQ^T += K^T dS^T, and the row sums of dS
-// correct D for the dK / dV kernel.  Its shape is the forward's, because a windowed item is
-// short (19 key blocks with a window of 1024): two workgroups of four waves per CU, so
-// that one loads its rows and writes its results while the other computes.  Each wave takes
-// both 32-key halves of a block for its (query head, 32 rows); halves that no row of the wave
-// attends are passed over.  With one workgroup of eight waves per CU, as in the causal kernel, every CU waited
-// about 10 of an item's 36 us for its rows (32K tokens, 32 heads, window 1024: 1146 us).
+// correct D for the dK / dV kernel.  dS is rounded to bf16 for its product with K, as in the
+// causal kernel: K is bf16, and half a step of each term is what the bf16 dQ has itself.
+//
+// Its shape is the forward's, because a windowed item is short (19 key blocks with a window
+// of 1024): two workgroups of four waves per CU, so that one loads its rows and writes its
+// results while the other computes.  Each wave takes both 32-key halves of a block for its
+// (query head, 32 rows); halves that no row of the wave attends are passed over.  With one
+// workgroup of eight waves per CU, as in the causal kernel, every CU waited about 10 of an
+// item's 36 us for its rows: 1146 us for 32K tokens, 32 heads, window 1024, now 870.
+// Bound by the three products (741 GFLOP there, 850 TFLOP/s) at the clock that the card
+// holds under them: the matrix cores are busy half of the cycles, at 1.77 GHz.
 //
 // The kernel also does what the causal calls leave to a pass of its own over Q, O and dO:
 // D = rowsum(dO O), and the records of the dK / dV kernel (see pre_pass in attn_bwd.hip for

