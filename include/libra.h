@@ -297,6 +297,8 @@ int libra_attn_bwd(const void *q, const void *k, const void *v, const void *o, c
  * of at least the longest sample gives causal attention.
  *   window >= 1; 0 <= sinks <= 1024 (EUNSUPPORTED above).  Values past
  *       n_kv_rows act as n_kv_rows.  The backward takes those of the forward.
+ *   Tensors are 16-byte aligned, lse, cu_seqlens and tiles to their elements
+ *       (else EINVAL).
  *   All other arguments, layouts, flags, errors, the handling of tiles that
  *       are out of range and the timing records: as in libra_attn_fwd and
  *       libra_attn_bwd.
@@ -378,6 +380,8 @@ typedef struct libra_ckpt8 {
  *   lse: fp32, of the forward on the values before packing.
  *   workspace: >= libra_attn_bwd_ckpt8_workspace_size bytes, 256-byte aligned
  *       (the unpacked tensors, then a backward's workspace).
+ *   dout, dq, dk and dv are 16-byte aligned, lse, cu_seqlens and tiles to their
+ *       elements (else EINVAL).
  * Everything else as in libra_attn_bwd.
  */
 size_t libra_attn_bwd_ckpt8_workspace_size(int64_t num_tiles, int64_t num_samples,

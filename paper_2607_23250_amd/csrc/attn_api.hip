@@ -4,6 +4,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <mutex>
 #include <vector>
 
@@ -78,6 +79,18 @@ int check_window(int64_t window, int64_t sinks, int64_t n_kv, Window *out) {
     return fail(LIBRA_EUNSUPPORTED, "%lld sinks (at most %d)", (long long)sinks, kMaxSinks);
   out->size = (int32_t)(window < n_kv ? window : n_kv);
   out->sinks = (int32_t)(sinks < n_kv ? sinks : n_kv);
+  return LIBRA_OK;
+}
+
+// The kernels move 16 bytes at a time; offsets and tiles are read as 8-byte words.
+int check_aligned(std::initializer_list<const void *> tensors, const float *lse,
+                  const int64_t *cu, const libra_tile_t *tiles) {
+  uintptr_t low = 0;
+  for (const void *p : tensors) low |= reinterpret_cast<uintptr_t>(p);
+  if (low % 16) return fail(LIBRA_EINVAL, "tensors must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(lse) % 4 || reinterpret_cast<uintptr_t>(cu) % 8 ||
+      reinterpret_cast<uintptr_t>(tiles) % 8)
+    return fail(LIBRA_EINVAL, "lse, cu_seqlens or tiles not aligned to their elements");
   return LIBRA_OK;
 }
 
@@ -245,6 +258,7 @@ extern "C" int libra_attn_window_fwd(const void *q, const void *k, const void *v
   Window win;
   if (int rc = check_sizes(num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim)) return rc;
   if (int rc = check_window(window, sinks, n_kv_rows, &win)) return rc;
+  if (int rc = check_aligned({q, k, v, o}, lse, cu_seqlens, tiles)) return rc;
   return attn_fwd(q, k, v, cu_seqlens, num_samples, tiles, num_tiles, n_q_rows, n_kv_rows, h_q,
                   h_kv, head_dim, softmax_scale, o, lse, workspace, workspace_bytes, stream, win);
 }
@@ -326,6 +340,7 @@ extern "C" int libra_attn_window_bwd(const void *q, const void *k, const void *v
   if (int rc = check_window(window, sinks, n_kv_rows, &win)) return rc;
   if (int rc = check_bwd(q, k, v, o, lse, dout, cu_seqlens, tiles, num_tiles, dq, dk, dv, flags))
     return rc;
+  if (int rc = check_aligned({q, k, v, o, dout, dq, dk, dv}, lse, cu_seqlens, tiles)) return rc;
   const BwdLayout L =
       bwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, win);
   if (num_tiles > 0)
@@ -429,6 +444,7 @@ extern "C" int libra_attn_bwd_ckpt8(const libra_ckpt8_t *q, const libra_ckpt8_t 
     if (int rc = check_window(window, sinks, n_kv_rows, &win)) return rc;
   if (int rc = check_bwd(q, k, v, o, lse, dout, cu_seqlens, tiles, num_tiles, dq, dk, dv, flags))
     return rc;
+  if (int rc = check_aligned({dout, dq, dk, dv}, lse, cu_seqlens, tiles)) return rc;
   const Ckpt8Layout C =
       ckpt8_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, win);
   char *ws = static_cast<char *>(workspace);

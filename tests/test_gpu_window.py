@@ -408,6 +408,32 @@ def _results_in(bufs):
     return [o, lse, dq, dk, dv, *(t for p in held for t in p), dq8, dk8, dv8]
 
 
+def test_two_calls_at_once():
+    """Layers on two streams with workspaces of their own, posted without waiting."""
+    h_q, h_kv, d, lengths, mask = 16, 4, 128, [2500, 900, 64], dict(window=300, sinks=3)
+    n = sum(lengths)
+    say(f"[two at once] lengths={lengths}")
+    tiles = blocks(n, 512, h_q, 2)
+    cu, td = offsets(lengths), pl.tiles_to_device(tiles, DEV)
+    sets = [dev(*tensors(s, n, n, h_q, h_kv, d)) for s in (3, 4)]
+    bufs = [_buffers(*t[:2], len(tiles), len(lengths), mask) for t in sets]
+    want = []
+    for t, b in zip(sets, bufs):
+        _step(*t, cu, td, mask, b)
+        want.append(_results(b))
+        for x in _results_in(b):
+            x.zero_()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(3):
+        for st, t, b in zip(streams, sets, bufs):
+            with torch.cuda.stream(st):
+                _step(*t, cu, td, mask, b)
+    torch.cuda.synchronize()
+    for b, w in zip(bufs, want):
+        assert all(torch.equal(x, y) for x, y in zip(w, _results(b)))
+
+
 def test_wide_window_is_causal():
     """A window of the longest sample: causal attention, within both calls' bounds."""
     h_q, h_kv, d, lengths = 8, 2, 128, [700, 64, 300]

@@ -78,6 +78,29 @@ def test_attention_refusals_of_one_direction():
     assert bwd8(held=(4097, 4096)) == pl.LIBRA_EINVAL
 
 
+@pytest.mark.parametrize("call", ["fwd", "bwd", "bwd8"])
+def test_misaligned_pointers(call):
+    """Each pointer in turn off by less than its alignment."""
+    L, c = pl.lib(), C.byref(pl._Ckpt8(4096, 4096))
+    names = {"fwd": "q k v cu tiles o lse".split(), "bwd8": "lse do cu tiles dq dk dv".split(),
+             "bwd": "q k v o lse do cu tiles dq dk dv".split()}[call]
+    for bad in names:
+        off = {"lse": 2, "cu": 4, "tiles": 4}.get(bad, 8)
+        p = {n: C.c_void_p(4096 + (off if n == bad else 0)) for n in names}
+        if call == "fwd":
+            rc = L.libra_attn_window_fwd(p["q"], p["k"], p["v"], p["cu"], 1, p["tiles"], 1, 10, 10,
+                                         4, 2, 64, 5, 0, 0.0, p["o"], p["lse"], FAKE, 1 << 40, None)
+        elif call == "bwd":
+            rc = L.libra_attn_window_bwd(p["q"], p["k"], p["v"], p["o"], p["lse"], p["do"], p["cu"],
+                                         1, p["tiles"], 1, 10, 10, 4, 2, 64, 5, 0, 0.0, p["dq"],
+                                         p["dk"], p["dv"], 0, FAKE, 1 << 40, None)
+        else:
+            rc = L.libra_attn_bwd_ckpt8(c, c, c, c, p["lse"], p["do"], p["cu"], 1, p["tiles"], 1,
+                                        10, 10, 4, 2, 64, 5, 0, 0.0, p["dq"], p["dk"], p["dv"], 0,
+                                        FAKE, 1 << 40, None)
+        assert rc == pl.LIBRA_EINVAL and b"aligned" in L.libra_last_error(), bad
+
+
 @pytest.mark.parametrize("name", ["pack", "unpack"])
 def test_ckpt8_refusals(name):
     def call(dtype=0, rows=4, cols=64, ld=64, x=FAKE, q=FAKE, e=FAKE):
