@@ -831,7 +831,7 @@ __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 
     const int64_t full_len = cu[item.sample + 1] - key0;
     // keys past the last covered row get no gradient
     const int64_t len = WIN ? (int64_t)samples[item.sample].ext : full_len;
-    const bool far = WIN && far_sample(win, full_len);   // its sinks' far rows are not walked here
+    const bool far = WIN && far_sample(win, full_len, n_kv - key0);   // its sinks' far rows are not walked here
     const int near_sinks = far ? 0 : win.sinks;
     const int g = item.g;
     const int kloc0 = item.kb * kBwdBK;

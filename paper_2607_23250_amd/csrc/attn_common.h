@@ -276,8 +276,10 @@ __device__ __forceinline__ bf16x8 held8(const Held &x, size_t at) {
 // (Backward of 4096 tokens, 8 / 2 heads, window 256, 4 sinks: 196 us with 512, 157 with 256 and
 // 128; of 8192, 32 / 4 heads, window 512: 794 with 2048, 474, 449, 446.)
 constexpr int kFarRows = 256;
-__host__ __device__ __forceinline__ bool far_sample(const Window &w, int64_t len) {
-  return w.sinks > 0 && len > (int64_t)w.size + kFarRows;
+// `keys`: those from its first to the end of K, which the last sample may pass; the
+// workspace has room for the far samples that fit K side by side.
+__device__ __forceinline__ bool far_sample(const Window &w, int64_t len, int64_t keys) {
+  return w.sinks > 0 && (len < keys ? len : keys) > (int64_t)w.size + kFarRows;
 }
 // The item walks its key blocks as steps: `far` blocks of sinks from key 0 on,
 // then, `gap` blocks later, those of the window.

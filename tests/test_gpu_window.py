@@ -434,6 +434,24 @@ def test_two_calls_at_once():
         assert all(torch.equal(x, y) for x, y in zip(w, _results(b)))
 
 
+def test_last_sample_past_the_keys():
+    """Offsets of a sample that goes on behind the last row of K and V: as if it ended there."""
+    h_q, h_kv, d, n, mask = 4, 2, 64, 1200, dict(window=900, sinks=4)
+    say("[window, last sample past the keys]")
+    tiles = blocks(n, 256, h_q)
+    q, k, v, do = tensors(9, n, n, h_q, h_kv, d)
+    cu = torch.tensor([0, 200, 50000], device=DEV)
+    qd, kd, vd, dod = dev(q, k, v, do)
+    td = pl.tiles_to_device(tiles, DEV)
+    want = ref.attention(q, k, v, ref.visible([200, 1000], ref.positions(tiles), n, 900, 4),
+                         torch.ones((n, h_q), dtype=torch.bool), dout=do)
+    o, lse = pl.libra_attn_window_fwd(qd, kd, vd, cu, td, **mask)
+    got = (o, lse, *pl.libra_attn_window_bwd(qd, kd, vd, o, lse, dod, cu, td, **mask))
+    torch.cuda.synchronize()
+    for name, x in zip(("o", "lse", "dq", "dk", "dv"), got):
+        ref.close(name, x, want[name])
+
+
 def test_wide_window_is_causal():
     """A window of the longest sample: causal attention, within both calls' bounds."""
     h_q, h_kv, d, lengths = 8, 2, 128, [700, 64, 300]
