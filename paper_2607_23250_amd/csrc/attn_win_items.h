@@ -501,9 +501,10 @@ struct WinSink {
   int32_t base, parts;
 };
 constexpr int kMaxSinks = 1024;
-// Rows of a part of far rows at least (backward of 8192 tokens, 32 / 4 heads, window 512,
-// 4 sinks: 500 us with 512, 465 with 128 and with 32).
-constexpr int kSinkPartRows = 128;
+// Rows of a part of far rows at least (backward with 4 sinks: 8192 tokens, 32 / 4 heads, window
+// 512: 500 us with 512, 465 with 128 and with 32; 2000 tokens, 8 / 2 heads, window 256: 119 with
+// 128, 114 with 32).
+constexpr int kSinkPartRows = 32;
 constexpr int kSinkParts = 256;      // slots beyond one for each WinSink
 __host__ __device__ constexpr int sink_blocks(const Window &w) { return (w.sinks + 31) / 32; }
 __host__ __device__ constexpr size_t sink_part_floats(int d) { return (size_t)2 * 32 * d; }
@@ -538,11 +539,14 @@ struct WinBwdPrep {
   int parts;
 };
 // Row ranges of a dK / dV item.  A call of few key blocks and KV heads (4K tokens and 2 KV
-// heads: 66 items for 256 CUs) cuts each into as many as the CUs hold, of at least 8 row blocks,
-// and up to 8 (2 / 1 heads, window 4096: 145 us; 163 with up to 4; no less with 16).
+// heads: 66 items for 256 CUs) cuts each into as many as the CUs hold, of at least 2 row blocks
+// (backward of 1000 tokens, 4 / 1 heads, window 300: 106 us with at least 8, 81 with 4, 77 with
+// 2), and up to 8 (4096 tokens, 2 / 1 heads, window 4096: 145 us; 163 with up to 4; no less
+// with 16).
+constexpr int kWinKvMinBlocks = 2;
 inline int win_kv_parts(const Window &w, int64_t key_blocks, int h_kv, int cus) {
   const int64_t fit = cus / (key_blocks * h_kv);
-  const int64_t most = ((int64_t)w.size + kBwdBK) / (kBwdSplitMinBlocks * kRows);
+  const int64_t most = ((int64_t)w.size + kBwdBK) / (kWinKvMinBlocks * kRows);
   const int64_t n = fit < most ? fit : most;
   return (int)(n < 1 ? 1 : n > 8 ? 8 : n);
 }
