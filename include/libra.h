@@ -196,10 +196,11 @@ int libra_attn_fwd(const void *q, const void *k, const void *v, const int64_t *c
  * q_end > n_kv_rows, empty ranges, rows past n_q_rows, heads outside
  * [0, h_q)) are skipped on the device: the call still returns LIBRA_OK and
  * computes every other tile exactly as without them.  The number skipped by
- * the last libra_attn_fwd or libra_attn_bwd call that used a workspace is an
- * int32 at byte offset LIBRA_WS_SKIPPED_OFFSET of that workspace (plus 1 if
- * the workspace's work-item list overflowed, which a workspace of
- * libra_attn_workspace_size bytes rules out).
+ * the last libra_attn_fwd or libra_attn_bwd call (windowed and checkpoint ones
+ * too) that used a workspace is an int32 at byte offset
+ * LIBRA_WS_SKIPPED_OFFSET of that workspace (plus 1 if the workspace's
+ * work-item list overflowed, which a workspace of the call's own size function
+ * rules out).
  *
  * libra_attn_skipped_tiles -- copies that count to *count after the work
  * already enqueued on `stream` has finished (it synchronizes `stream`).
@@ -379,7 +380,7 @@ typedef struct libra_ckpt8 {
  * need not sum to 1).
  *   lse: fp32, of the forward on the values before packing.
  *   workspace: >= libra_attn_bwd_ckpt8_workspace_size bytes, 256-byte aligned
- *       (the unpacked tensors, then a backward's workspace).
+ *       (a backward's workspace, then the unpacked tensors).
  *   dout, dq, dk and dv are 16-byte aligned, lse, cu_seqlens and tiles to their
  *       elements (else EINVAL).
  * Everything else as in libra_attn_bwd.

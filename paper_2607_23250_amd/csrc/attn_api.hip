@@ -374,10 +374,11 @@ int check_ckpt8(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_
   return LIBRA_OK;
 }
 
-// Workspace of libra_attn_bwd_ckpt8: the unpacked k and v, for a causal call q and o too
-// (the windowed kernels read them as they are), then a backward's.
+// Workspace of libra_attn_bwd_ckpt8: a backward's, whose header is at its start as in the
+// other calls, then the unpacked k and v, for a causal call q and o too (the windowed
+// kernels read them as they are).
 struct Ckpt8Layout {
-  size_t at[4], bwd = 0, total = 0;
+  size_t at[4], total = 0;
   BwdLayout L;
 };
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
@@ -387,12 +388,11 @@ Ckpt8Layout ckpt8_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_
   c.L = bwd_layout(T, n, n_q, n_kv, h_q, h_kv, d, win);
   const size_t q = win.size ? 0 : align256((size_t)n_q * h_q * d * 2);
   const size_t k = align256((size_t)n_kv * h_kv * d * 2);
-  c.at[0] = 0;
-  c.at[1] = q;
-  c.at[2] = q + k;
-  c.at[3] = q + 2 * k;
-  c.bwd = 2 * q + 2 * k;
-  c.total = c.bwd + c.L.total;
+  c.at[0] = align256(c.L.total);
+  c.at[1] = c.at[0] + q;
+  c.at[2] = c.at[1] + k;
+  c.at[3] = c.at[2] + k;
+  c.total = c.at[3] + q;
   return c;
 }
 
@@ -469,6 +469,6 @@ extern "C" int libra_attn_bwd_ckpt8(const libra_ckpt8_t *q, const libra_ckpt8_t 
   return attn_bwd(as_held ? nullptr : ws + C.at[0], ws + C.at[1], ws + C.at[2],
                   as_held ? nullptr : ws + C.at[3], lse, dout, cu_seqlens, num_samples, tiles,
                   num_tiles, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, softmax_scale, dq, dk, dv,
-                  flags, num_tiles > 0 ? ws + C.bwd : ws, C.L, stream, false, win,
+                  flags, ws, C.L, stream, false, win,
                   as_held ? Held{q->q, q->e} : Held{}, as_held ? Held{o->q, o->e} : Held{});
 }
