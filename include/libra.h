@@ -378,6 +378,9 @@ typedef struct libra_ckpt8 {
  * D = rowsum(dO * O), for dQ and for dK alike (libra_attn_bwd, whose O and LSE
  * belong to its q, k and v, corrects D by the sums of dS; here the rows of P
  * need not sum to 1).
+ * Nor is P bounded by 1: where it or dS passes the range of fp16, the dK / dV
+ * products concerned are formed again with P and dS in bf16 pairs (16 bits, the
+ * range of fp32, past which a gradient is infinite or NaN).
  *   lse: fp32, of the forward on the values before packing.
  *   workspace: >= libra_attn_bwd_ckpt8_workspace_size bytes, 256-byte aligned
  *       (a backward's workspace, then the unpacked tensors).

@@ -769,7 +769,9 @@ __global__ __launch_bounds__(256) void bwd_copy_kernel(BwdPass a) {
 // keys of a sample that is not a far one, with the sample); the rows that a key's
 // window leaves out are masked like those before it.  The sums of a far sample's sinks
 // over the rows past their windows come from win_sink_kernel and are added at the end.
-template <int D, bool WIN>
+// LOOSE: LSE is not that of q and k; items whose sums leave the fp16 range are redone
+// (attn_bwd_steps.h).
+template <int D, bool WIN, bool LOOSE>
 __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 1))) void attn_bwd_dkdv_kernel(
     const f16 *__restrict__ k, const f16 *__restrict__ v, const f16 *__restrict__ rec,
     const int64_t *__restrict__ cu, const libra_tile_t *__restrict__ tiles, int64_t T,
@@ -781,6 +783,7 @@ __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 
   using S = KvShape<D>;
   extern __shared__ __attribute__((aligned(16))) bf16 smem[];
   __shared__ int32_t s_item;
+  __shared__ int32_t s_wide;   // LOOSE: the item is to be redone
 
   const int tid = threadIdx.x, l = tid & 63, ln = l & 31, kg = l >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);   // wave index (uniform)
@@ -822,6 +825,8 @@ __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 
       const int got = WIN ? take_run_item(hdr, kBwdQ, q_serve, q_state)
                           : take_item(hdr, kBwdQ, q_serve, q_state);
       if (tid == 0) s_item = got;
+      if constexpr (LOOSE)
+        if (tid == 0) s_wide = 0;
     }
     __syncthreads();
     const int idx = __builtin_amdgcn_readfirstlane(s_item);
@@ -1164,6 +1169,38 @@ __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 
       steps(std::true_type{});
     }
 
+    if constexpr (LOOSE) {
+      if (__builtin_amdgcn_ballot_w64(not_finite(dka) || not_finite(dva)) && l == 0) s_wide = 1;
+      wait_vm_n<0>();
+      __syncthreads();
+      if (__builtin_expect(s_wide, 0)) {
+        static_for<D / 32>([&](auto dt) {
+          dva[dt] = mfma_zero();
+          dka[dt] = mfma_zero();
+        });
+        StepIter<WIN> again{tiles, WIN ? (int64_t)item.t1 + 1 : T, n_q, n_kv, key0, key0 + item.r0,
+                     key0 + (item.r1 < len ? item.r1 : len), h_q, g, G, kloc0,
+                     2 * S::HEAD_EL / 1024};
+        constexpr uint32_t bytes = 2u * S::STAGE_EL / kWaves;
+        for (again.start(WIN ? item.t0 : 0); again.valid; again.next()) {
+          cp_dst = lds_addr(smem) + bytes * w;
+          cp_src = reinterpret_cast<const char *>(rec) + (uniform64(again.rec) << 10) + bytes * w;
+          copy_all();
+          wait_vm_n<0>();
+          __syncthreads();
+          const int qb = again.qb();
+          const int lower = max(kl - qb, again.lo());
+          int upper = key_ok ? again.hi() : 0;
+          if constexpr (WIN)
+            if (kl >= near_sinks) upper = min(upper, kl - qb + win.size);
+          for (int x = 0; x <= (int)again.two(); ++x)
+            wide_step<D>(smem + x * S::HEAD_EL, l, qoff, troff, ones3, kf, vf, c2s, lower - 8 * kg,
+                         upper - 8 * kg, dka, dva);
+          __syncthreads();   // the stage is read
+        }
+      }
+    }
+
     if constexpr (WIN) {
       // the far rows of this wave's sinks (places as written by win_sink_sum_kernel)
       const int first = samples[item.sample].far;   // -1: no far row is covered
@@ -1363,7 +1400,9 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
   f16 *v16 = reinterpret_cast<f16 *>(ws + L.v16);
   float *stats = reinterpret_cast<float *>(ws + L.stats);
   int32_t *cov = reinterpret_cast<int32_t *>(ws + L.cov);
-  if (int rc = reserve_lds<&attn_bwd_dkdv_kernel<D, WIN>>(KvShape<D>::SMEM)) return rc;
+  if (int rc = exact_o ? reserve_lds<&attn_bwd_dkdv_kernel<D, WIN, false>>(KvShape<D>::SMEM)
+                       : reserve_lds<&attn_bwd_dkdv_kernel<D, WIN, true>>(KvShape<D>::SMEM))
+    return rc;
   // bf16 dK / dV are written where a covered row attends and zero elsewhere
   const int64_t n16 = accumulate ? 0 : n_kv * h_kv * D * (int64_t)sizeof(bf16) / 16;
   const unsigned zero_blocks = (unsigned)std::min<int64_t>((n16 + 255) / 256, 4096);
@@ -1454,12 +1493,14 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
     float *sink_parts = reinterpret_cast<float *>(ws + L.sink_parts);
     if constexpr (WIN)
       if (L.far > 0)
-        if (int e = launch_win_sinks(D, k16, v16, rec, wb, scale * kLog2e, sink_parts, cus, st))
+        if (int e = launch_win_sinks(D, !exact_o, k16, v16, rec, wb, scale * kLog2e, sink_parts,
+                                     cus, st))
           return e;
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(attn_bwd_dkdv_kernel<D, WIN>), dim3(cus), dim3(kThreads),
-                       KvShape<D>::SMEM, st, k16, v16, rec, cu, tiles, T, items, hdr, h_q, h_kv,
-                       n_q, n_kv, scale, scale * kLog2e, dk, dv, accumulate ? 1 : 0, parts, win,
-                       samples, wb.sinks, sink_parts);
+    hipLaunchKernelGGL((exact_o ? attn_bwd_dkdv_kernel<D, WIN, false>
+                                : attn_bwd_dkdv_kernel<D, WIN, true>),
+                       dim3(cus), dim3(kThreads), KvShape<D>::SMEM, st, k16, v16, rec, cu, tiles, T,
+                       items, hdr, h_q, h_kv, n_q, n_kv, scale, scale * kLog2e, dk, dv,
+                       accumulate ? 1 : 0, parts, win, samples, wb.sinks, sink_parts);
     if (WIN ? wb.parts > 1 : may_split_rows(n_kv))
       hipLaunchKernelGGL(HIP_KERNEL_NAME(bwd_dkdv_combine_kernel<D, WIN>), dim3(cus * 4),
                          dim3(256), 0, st,

@@ -34,6 +34,70 @@ struct KvShape {
   static_assert((NSTAGE - 2) * LOADS <= 63, "vmcnt range");
 };
 
+// The kernels that sum dK and dV hold P and dS in fp16.  That is enough where LSE is that
+// of q and k: P is at most 1 and, with max |dO| and max |V| scaled to [1, 2), |dP - D| below
+// 2^11.  In a backward from 8-bit checkpoints (LOOSE) LSE is that of q and k before they were
+// rounded, and P = exp(S - LSE) has no such bound: scores of some hundreds move by 10 and
+// more, and above 65504 the sums turn infinite or NaN and stay so.  Sums that ended so are
+// formed once more by wide_step.  (The look at them: causal backward of 4096 tokens, 8 / 2
+// heads, d = 64, 124.5 us without and 126.6 with it; of 32768, 32 / 8 heads, 10.2 and 10.1 ms.)
+template <int N>
+__device__ __forceinline__ bool not_finite(const f32x16 (&x)[N]) {
+  bool r = false;
+  static_for<N>([&](auto i) {
+    static_for<16>([&](auto e) { r |= !(fabsf(x[i][int(e)]) < INFINITY); });
+  });
+  return r;
+}
+// dV += dO^T P and dK += Q^T dS over the rows lower <= iq < upper (both less 8 kg) of one
+// record at Qs.  S and dP as in the kernels (their operands and offsets: see there); P and dS
+// as a bf16 number and a bf16 rest, 16 bits together and the range of fp32; Q^T and dO^T turned to
+// bf16, which holds them (they were bf16, scaled by a power of two).
+template <int D>
+__device__ __forceinline__ void wide_step(const bf16 *Qs, int l, const int (&qoff)[2],
+                                          const int (&troff)[2], const f16x8 &ones3,
+                                          const f16x8 (&kf)[D / 16], const f16x8 (&vf)[D / 16],
+                                          float c2s, int lower, int upper, f32x16 (&dka)[D / 32],
+                                          f32x16 (&dva)[D / 32]) {
+  constexpr int Q_EL = kRows * D;
+  const bf16 *Ag = Qs + 2 * Q_EL + 8 * l;
+  const bf16 *rp[2] = {Qs + qoff[0], Qs + qoff[1]};
+  const f16 *tp[2] = {reinterpret_cast<const f16 *>(Qs) + troff[0],
+                      reinterpret_cast<const f16 *>(Qs) + troff[1]};
+  f32x16 sa = mfma32h(*reinterpret_cast<const f16x8 *>(Ag), ones3, mfma_zero_c());
+  f32x16 pa = mfma32h(*reinterpret_cast<const f16x8 *>(Ag + kAugEl / 2), ones3, mfma_zero_c());
+  static_for<D / 16>([&](auto c) {
+    sa = mfma32h(*reinterpret_cast<const f16x8 *>(rp[c & 1] + 1024 * (c >> 1)), kf[c], sa);
+    pa = mfma32h(*reinterpret_cast<const f16x8 *>(rp[c & 1] + Q_EL + 1024 * (c >> 1)), vf[c], pa);
+  });
+  bf16x8 p16[2][2], s16[2][2];   // [rest][16 rows]
+  static_for<16>([&](auto r) {
+    constexpr int iq = 16 * (r >> 3) + (r & 7);
+    const float p = fast_exp2(iq >= lower && iq < upper ? sa[int(r)] * c2s : -INFINITY);
+    const float s = p * pa[int(r)];
+    p16[0][r >> 3][r & 7] = static_cast<bf16>(p);
+    s16[0][r >> 3][r & 7] = static_cast<bf16>(s);
+    p16[1][r >> 3][r & 7] = static_cast<bf16>(p - static_cast<float>(p16[0][r >> 3][r & 7]));
+    s16[1][r >> 3][r & 7] = static_cast<bf16>(s - static_cast<float>(s16[0][r >> 3][r & 7]));
+  });
+  auto turned = [&](int at) {
+    const f16x8 x = lds_tr16x2h(tp[0] + at, tp[1] + at);
+    bf16x8 y;
+    static_for<8>([&](auto i) { y[int(i)] = static_cast<bf16>(static_cast<float>(x[int(i)])); });
+    return y;
+  };
+  static_for<D / 32>([&](auto dt) {
+    static_for<2>([&](auto c) {
+      constexpr int at = 128 * c + 1024 * dt;
+      const bf16x8 o = turned(Q_EL + at), q = turned(at);
+      static_for<2>([&](auto rest) {
+        dva[dt] = mfma32(o, p16[rest][c], dva[dt]);
+        dka[dt] = mfma32(q, s16[rest][c], dka[dt]);
+      });
+    });
+  });
+}
+
 // Walks the steps (32-row query block x two query heads) that attend one KV
 // block: tiles in list order, query blocks in row order, heads in order.  Per
 // fragment (one tile's rows of the sample) everything a step needs is

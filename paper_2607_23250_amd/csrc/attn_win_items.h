@@ -590,8 +590,9 @@ int launch_win_dq(int d, const WinDq &a, int cus, hipStream_t st);
 void launch_win_prep_fwd(const WinPrep &p, hipStream_t st);
 // The preparation of a windowed backward: the dQ items (q) and the dK / dV items (b).
 void launch_win_prep_bwd(const WinPrep &q, const WinBwdPrep &b, int grid_kv, hipStream_t st);
-// The far rows of sink keys: partial sums of dK and dV, one slot a WinSink after it.
-int launch_win_sinks(int d, const f16 *k16, const f16 *v16, const f16 *rec, const WinBwdPrep &b,
-                     float c2, float *parts, int cus, hipStream_t st);
+// The far rows of sink keys: partial sums of dK and dV, one slot a WinSink after it.  `loose`:
+// see attn_bwd_steps.h.
+int launch_win_sinks(int d, bool loose, const f16 *k16, const f16 *v16, const f16 *rec,
+                     const WinBwdPrep &b, float c2, float *parts, int cus, hipStream_t st);
 
 }  // namespace libra

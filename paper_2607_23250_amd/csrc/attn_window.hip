@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "attn_bwd_steps.h"
 #include "attn_common.h"
@@ -278,7 +279,8 @@ void launch_win_prep_bwd(const WinPrep &q, const WinBwdPrep &b, int grid_kv, hip
 // added up.  With few sinks one of the 32 columns in eight or so counts, so the products do
 // not matter; bound by the latency of the records (a 32K pack with a 16K sample, 32 / 8 heads:
 // 250 MB in 117 us, one workgroup to a CU).
-template <int D>
+// LOOSE: as in the dK / dV kernel.
+template <int D, bool LOOSE>
 __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 1))) void
 win_sink_kernel(const f16 *__restrict__ k, const f16 *__restrict__ v,
                 const f16 *__restrict__ rec, WinBwdPrep a, float c2,
@@ -325,85 +327,96 @@ win_sink_kernel(const f16 *__restrict__ k, const f16 *__restrict__ v,
     });
     wait_vm_known();
     f32x16 dva[NT], dka[NT];
-    static_for<NT>([&](auto dt) {
-      dva[dt] = mfma_zero_c();
-      dka[dt] = mfma_zero_c();
-    });
-    StepIter<true> it{a.tiles, (int64_t)item.t1 + 1, a.n_q, a.n_kv, key0, key0 + item.r0,
-                key0 + item.r1, a.h_q, item.g, G, 0, 2 * S::HEAD_EL / 1024};
-    it.start(item.t0);
-    // this wave's units: the heads of every fourth step, the copy of the next one under way
-    // while one is computed
-    int n = 0, hb = 0;
-    auto skip = [&]() {   // to the next step of this wave
-      for (; it.valid && (n & (kWaves - 1)) != w; ++n) it.next();
-    };
-    struct Unit {
-      int lower, upper;   // rows of the block that count for this lane's key, less 8 kg
-    };
-    auto copy = [&](int buf) {
-      const int qb = it.qb(), first = kl + a.win.size - qb;   // first row past the window
-      const Unit u{max(it.lo(), min(first, kRows)) - 8 * kg, (key_ok ? it.hi() : 0) - 8 * kg};
-      const char *src = reinterpret_cast<const char *>(rec) +
-                        (uniform64(it.rec + hb * (S::HEAD_EL / 512)) << 10);
-      const uint32_t dst = stage_at + (uint32_t)(buf * S::HEAD_EL * sizeof(bf16));
-      static_for<LOADS / 4>([&](auto i) { g2l_run<4>(src + 4096 * i, 16u * l, dst + 4096u * i); });
-      if constexpr (LOADS % 4 != 0)
-        g2l_run<LOADS % 4>(src + LOADS / 4 * 4096, 16u * l, dst + LOADS / 4 * 4096u);
-      if (hb == 0 && it.two()) {
-        hb = 1;
-      } else {
-        hb = 0;
-        it.next();
-        ++n;
-        skip();
-      }
-      return u;
-    };
-    skip();
-    bool more = it.valid;
-    Unit next{};
-    if (more) next = copy(0);
-    for (int buf = 0; more; buf ^= 1) {
-      const Unit u = next;
-      more = it.valid;
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the other stage's reads are done
-      if (more) {
-        next = copy(buf ^ 1);
-        wait_vm_n<LOADS>();
-      } else {
-        wait_vm();
-      }
-      const bf16 *Qs = stage + buf * S::HEAD_EL;
-      const bf16 *Ag = Qs + 2 * S::Q_EL + 8 * l;
-      const bf16 *rp[2] = {Qs + qoff[0], Qs + qoff[1]};
-      const f16 *tp[2] = {reinterpret_cast<const f16 *>(Qs) + troff[0],
-                          reinterpret_cast<const f16 *>(Qs) + troff[1]};
-      f32x16 sa = mfma32h(*reinterpret_cast<const f16x8 *>(Ag), ones3, mfma_zero_c());
-      f32x16 pa =
-          mfma32h(*reinterpret_cast<const f16x8 *>(Ag + kAugEl / 2), ones3, mfma_zero_c());
-      static_for<NC>([&](auto c) {
-        sa = mfma32h(*reinterpret_cast<const f16x8 *>(rp[c & 1] + 1024 * (c >> 1)), kf[c], sa);
-        pa = mfma32h(*reinterpret_cast<const f16x8 *>(rp[c & 1] + S::Q_EL + 1024 * (c >> 1)),
-                     vf[c], pa);
-      });
-      f16x8 p16[2], s16[2];
-      static_for<16>([&](auto r) {
-        constexpr int iq = 16 * (r >> 3) + (r & 7);
-        const float x = iq >= u.lower && iq < u.upper ? sa[int(r)] * c2s : -INFINITY;
-        const float p = fast_exp2(x);
-        p16[r >> 3][r & 7] = static_cast<f16>(p);
-        s16[r >> 3][r & 7] = static_cast<f16>(p * pa[int(r)]);
-      });
+    // sums this wave's part; WIDE: whatever the size of P
+    auto sum_up = [&](auto wide_t) {
+      constexpr bool WIDE = decltype(wide_t)::value;
       static_for<NT>([&](auto dt) {
-        static_for<2>([&](auto c) {
-          constexpr int at = 128 * c + 1024 * dt;
-          dva[dt] = mfma32h(lds_tr16x2h(tp[0] + S::Q_EL + at, tp[1] + S::Q_EL + at), p16[c],
-                            dva[dt]);
-          dka[dt] = mfma32h(lds_tr16x2h(tp[0] + at, tp[1] + at), s16[c], dka[dt]);
-        });
+        dva[dt] = mfma_zero_c();
+        dka[dt] = mfma_zero_c();
       });
-    }
+      StepIter<true> it{a.tiles, (int64_t)item.t1 + 1, a.n_q, a.n_kv, key0, key0 + item.r0,
+                  key0 + item.r1, a.h_q, item.g, G, 0, 2 * S::HEAD_EL / 1024};
+      it.start(item.t0);
+      // this wave's units: the heads of every fourth step, the copy of the next one under way
+      // while one is computed
+      int n = 0, hb = 0;
+      auto skip = [&]() {   // to the next step of this wave
+        for (; it.valid && (n & (kWaves - 1)) != w; ++n) it.next();
+      };
+      struct Unit {
+        int lower, upper;   // rows of the block that count for this lane's key, less 8 kg
+      };
+      auto copy = [&](int buf) {
+        const int qb = it.qb(), first = kl + a.win.size - qb;   // first row past the window
+        const Unit u{max(it.lo(), min(first, kRows)) - 8 * kg, (key_ok ? it.hi() : 0) - 8 * kg};
+        const char *src = reinterpret_cast<const char *>(rec) +
+                          (uniform64(it.rec + hb * (S::HEAD_EL / 512)) << 10);
+        const uint32_t dst = stage_at + (uint32_t)(buf * S::HEAD_EL * sizeof(bf16));
+        static_for<LOADS / 4>([&](auto i) { g2l_run<4>(src + 4096 * i, 16u * l, dst + 4096u * i); });
+        if constexpr (LOADS % 4 != 0)
+          g2l_run<LOADS % 4>(src + LOADS / 4 * 4096, 16u * l, dst + LOADS / 4 * 4096u);
+        if (hb == 0 && it.two()) {
+          hb = 1;
+        } else {
+          hb = 0;
+          it.next();
+          ++n;
+          skip();
+        }
+        return u;
+      };
+      skip();
+      bool more = it.valid;
+      Unit next{};
+      if (more) next = copy(0);
+      for (int buf = 0; more; buf ^= 1) {
+        const Unit u = next;
+        more = it.valid;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the other stage's reads are done
+        if (more) {
+          next = copy(buf ^ 1);
+          wait_vm_n<LOADS>();
+        } else {
+          wait_vm();
+        }
+        const bf16 *Qs = stage + buf * S::HEAD_EL;
+        const bf16 *Ag = Qs + 2 * S::Q_EL + 8 * l;
+        const bf16 *rp[2] = {Qs + qoff[0], Qs + qoff[1]};
+        const f16 *tp[2] = {reinterpret_cast<const f16 *>(Qs) + troff[0],
+                            reinterpret_cast<const f16 *>(Qs) + troff[1]};
+        if constexpr (WIDE) {
+          wide_step<D>(Qs, l, qoff, troff, ones3, kf, vf, c2s, u.lower, u.upper, dka, dva);
+          continue;
+        }
+        f32x16 sa = mfma32h(*reinterpret_cast<const f16x8 *>(Ag), ones3, mfma_zero_c());
+        f32x16 pa =
+            mfma32h(*reinterpret_cast<const f16x8 *>(Ag + kAugEl / 2), ones3, mfma_zero_c());
+        static_for<NC>([&](auto c) {
+          sa = mfma32h(*reinterpret_cast<const f16x8 *>(rp[c & 1] + 1024 * (c >> 1)), kf[c], sa);
+          pa = mfma32h(*reinterpret_cast<const f16x8 *>(rp[c & 1] + S::Q_EL + 1024 * (c >> 1)),
+                       vf[c], pa);
+        });
+        f16x8 p16[2], s16[2];
+        static_for<16>([&](auto r) {
+          constexpr int iq = 16 * (r >> 3) + (r & 7);
+          const float x = iq >= u.lower && iq < u.upper ? sa[int(r)] * c2s : -INFINITY;
+          const float p = fast_exp2(x);
+          p16[r >> 3][r & 7] = static_cast<f16>(p);
+          s16[r >> 3][r & 7] = static_cast<f16>(p * pa[int(r)]);
+        });
+        static_for<NT>([&](auto dt) {
+          static_for<2>([&](auto c) {
+            constexpr int at = 128 * c + 1024 * dt;
+            dva[dt] = mfma32h(lds_tr16x2h(tp[0] + S::Q_EL + at, tp[1] + S::Q_EL + at), p16[c],
+                              dva[dt]);
+            dka[dt] = mfma32h(lds_tr16x2h(tp[0] + at, tp[1] + at), s16[c], dka[dt]);
+          });
+        });
+      }
+    };
+    sum_up(std::false_type{});
+    if constexpr (LOOSE)
+      if (__builtin_amdgcn_ballot_w64(not_finite(dka) || not_finite(dva))) sum_up(std::true_type{});
     // the waves' sums, each in its own stage, then added in wave order
     static_assert(2 * NT * 16 * 64 * sizeof(float) <= S::STAGE_EL * sizeof(bf16), "fits");
     float *ex = reinterpret_cast<float *>(stage);
@@ -453,20 +466,21 @@ __global__ __launch_bounds__(256) void win_sink_sum_kernel(const WinSink *__rest
   }
 }
 
-template <int D>
+template <int D, bool LOOSE>
 static int launch_sinks(const f16 *k16, const f16 *v16, const f16 *rec, const WinBwdPrep &b,
                         float c2, float *parts, int cus, hipStream_t st) {
-  if (int rc = reserve_lds<&win_sink_kernel<D>>(KvShape<D>::SMEM)) return rc;
-  hipLaunchKernelGGL(win_sink_kernel<D>, dim3(cus), dim3(kThreads), KvShape<D>::SMEM, st, k16,
-                     v16, rec, b, c2, parts);
+  if (int rc = reserve_lds<&win_sink_kernel<D, LOOSE>>(KvShape<D>::SMEM)) return rc;
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(win_sink_kernel<D, LOOSE>), dim3(cus), dim3(kThreads),
+                     KvShape<D>::SMEM, st, k16, v16, rec, b, c2, parts);
   hipLaunchKernelGGL(win_sink_sum_kernel<D>, dim3(cus * 2), dim3(256), 0, st, b.sinks, b.hdr,
                      parts);
   return LIBRA_OK;
 }
-int launch_win_sinks(int d, const f16 *k16, const f16 *v16, const f16 *rec, const WinBwdPrep &b,
-                     float c2, float *parts, int cus, hipStream_t st) {
-  return d == 128 ? launch_sinks<128>(k16, v16, rec, b, c2, parts, cus, st)
-                  : launch_sinks<64>(k16, v16, rec, b, c2, parts, cus, st);
+int launch_win_sinks(int d, bool loose, const f16 *k16, const f16 *v16, const f16 *rec,
+                     const WinBwdPrep &b, float c2, float *parts, int cus, hipStream_t st) {
+  const auto launch = d == 128 ? (loose ? launch_sinks<128, true> : launch_sinks<128, false>)
+                               : (loose ? launch_sinks<64, true> : launch_sinks<64, false>);
+  return launch(k16, v16, rec, b, c2, parts, cus, st);
 }
 
 }  // namespace libra

@@ -1,11 +1,13 @@
 """GPU tests of libra_attn_bwd_ckpt8 besides its gradients at ordinary sizes: what it leaves in
-its workspace."""
+its workspace, and scores that the 8 bits move far."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2607_23250_amd as pl
+import window_ref as ref
 from gpu_util import DEV, say
+from grad_bounds import gradients
 from test_gpu_window import blocks, offsets, tensors
 
 pytestmark = pytest.mark.gpu
@@ -52,3 +54,56 @@ def test_skipped_tiles_are_counted(window, sinks):
                                                window=window, sinks=sinks, workspace=ws))
         assert pl.libra_attn_skipped_tiles(ws) == skipped
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def outliers(size):
+    """q and k with one large channel each: it sets the unit of its 32 elements, so the others
+    round coarsely, and meets them in the scores."""
+    def change(q, k, v, do):
+        q, k = 2 * q, 2 * k
+        q[..., 3] += size
+        k[..., 17] += size
+        return q, k, v, do
+    return change
+
+
+LARGE = {   # seed, lengths, tiles, heads, d, window, sinks; items cut into row ranges or whole
+    "causal_cut": (6, [700, 60], blocks(760, 128, 4, 2), (4, 2), 128, 0, 0),
+    "causal_cut_odd": (10, [500], blocks(500, 500, 3), (3, 1), 64, 0, 0),
+    "causal_whole": (11, [140] * 12, blocks(1680, 512, 8), (8, 4), 64, 0, 0),
+    "window_cut": (6, [900, 77], blocks(977, 300, 4), (4, 1), 64, 120, 0),
+    "window_cut_odd_far": (5, [1300], blocks(1300, 256, 3), (3, 1), 128, 100, 40),
+    "window_whole_far": (10, [1500, 200], blocks(1700, 512, 20, 2), (20, 10), 64, 150, 8),
+}
+
+
+@pytest.mark.parametrize("name", LARGE)
+def test_large_scores(name, monkeypatch):
+    """Scores of some hundreds and outlier channels: the rounding of q and k moves scores by more
+    than 11, so that P = exp(S - LSE) passes what fp16 holds, and dV and dK with it."""
+    seed, lengths, tiles, (h_q, h_kv), d, window, sinks = LARGE[name]
+    say(f"[ckpt8 large scores {name}] lengths={lengths} heads=({h_q},{h_kv}) d={d} "
+        f"window={window} sinks={sinks}")
+    _, _, _, do, o, lse, held, cu, td = layer(seed, lengths, tiles, h_q, h_kv, d, window,
+                                              sinks, outliers(150.0))
+    q8, k8, v8, o8 = (pl.libra_ckpt8_unpack(*x, dtype=torch.float32).cpu() for x in held)
+    lse_h, do_h = lse.cpu(), do.cpu()
+    n = sum(lengths)
+    pairs = (ref.visible(lengths, ref.positions(tiles), n, window, sinks),
+             ref.coverage(tiles, n, h_q))
+    want = gradients(monkeypatch, q8, k8, v8, do_h, pairs, d ** -0.5, lse_h, (o8, lse_h))
+    # the largest P of each key, and of the far rows of sinks
+    top = torch.stack([(torch.exp((q8[:, h].double() @ k8[:, h * h_kv // h_q].double().T)
+                                  * d ** -0.5 - lse_h[h, :, None].double()) * pairs[0])
+                       for h in range(h_q)]).amax(0)
+    assert 65504 < float(top.max()) < 1e30
+    if sinks:
+        assert float(top[window + sinks:lengths[0], :sinks].max()) > 65504
+    results = []
+    for accumulate in (False, True, False):
+        results.append(pl.libra_attn_bwd_ckpt8(*held, lse, do, cu, td, window=window, sinks=sinks,
+                                               accumulate=accumulate))
+        for what, got in zip(("dq", "dk", "dv"), results[-1]):
+            value, bound = want[what]
+            ref.close(what, got, (value, bound + 2.0 ** -23 * value.abs()))
+    assert all(torch.equal(a, b) for a, b in zip(results[0], results[2]))
