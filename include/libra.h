@@ -264,7 +264,8 @@ int libra_attn_fwd_noalloc(const void *q, const void *k, const void *v,
  * Precision: the dK / dV products take fp16 copies of q, dout, k and v, each
  * scaled by a power of two from its max |x| over what the products read, so
  * that P and dS round to 11 significant bits instead of bf16's 8; the scales
- * are undone exactly on output.  dQ's products take the bf16 inputs.
+ * are undone exactly on output.  (A softmax_scale below ln(n_kv_rows) / 56000
+ * holds the copies of q and k lower, so that LSE / softmax_scale fits too.)  dQ's products take the bf16 inputs.
  * Inputs: every element of k and v in the samples the tiles touch, and of
  * q, dout, o and lse in the covered (row, head) pairs, must be finite.
  * Other rows of q, dout, o and lse are not read by the dK / dV products

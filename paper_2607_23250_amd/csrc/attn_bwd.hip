@@ -67,6 +67,7 @@ struct BwdPrep {
   int grid;
   BwdSplit *splits;
   int32_t *cov, *cov_sum;   // per key block and KV head (see prep_bwd)
+  ScoreTops tops;
 };
 constexpr int kExtLds = 1024;   // samples whose extents and head sets are kept in LDS
 constexpr int kMaxLong = 256;
@@ -125,7 +126,8 @@ __device__ __forceinline__ void prep_bwd(const BwdPrep &a, BwdPrepLds &lds) {
     // the skipped-tile count (counted here for the backward), the odd-heads
     // flag and the max |x| slots
     __hip_atomic_store(&hdr[tid == 0 ? (int)kBadTiles : tid == 1 ? (int)kOddHeads : kMaxAbs + tid - 2],
-                       0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                       tid == 2 ? a.tops.q : tid == 4 ? a.tops.k : 0, __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
   }
   __threadfence();
   __syncthreads();
@@ -1433,7 +1435,8 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
                       reinterpret_cast<int32_t *>(ws + L.far_list),
                       reinterpret_cast<BwdItem *>(ws + L.sink_items), cus,
                       reinterpret_cast<BwdSplit *>(ws + L.kv_splits),
-                      win_kv_parts(win, L.max_blocks / h_kv, h_kv, cus)};
+                      win_kv_parts(win, L.max_blocks / h_kv, h_kv, cus),
+                      score_tops(scale, std::min(n_kv, (int64_t)win.size + win.sinks))};
       launch_win_prep_bwd(WinPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, win, hdr, qitems,
                                   L.max_qitems, 0, cus * kWinDqPerCu, cus * kWinDqPerCu,
                                   max_parts, splits}, wb, cus, st);
@@ -1442,7 +1445,7 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
       hipLaunchKernelGGL(prep_bwd_kernel, dim3(2), dim3(kPrepThreads), 0, st,
                          BwdPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, hdr, ext, gmask, items,
                                  L.max_items, cus, reinterpret_cast<BwdSplit *>(ws + L.bsplits),
-                                 cov, cov + L.max_blocks},
+                                 cov, cov + L.max_blocks, score_tops(scale, n_kv)},
                          FwdPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, hdr, qitems, L.max_qitems,
                                  0, cus, cus, max_parts, 1, splits});
     }

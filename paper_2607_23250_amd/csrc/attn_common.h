@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <atomic>
+#include <cmath>
 #include <cstdint>
 #include <type_traits>
 
@@ -671,6 +672,21 @@ __host__ __device__ __forceinline__ float fp16_scale(uint32_t mx, bool up) {
   int k = up ? -e : (e > 2 ? -(e - 2) : 0);
   k = k < -126 ? -126 : (k > 126 ? 126 : k);
   return __builtin_bit_cast(float, (uint32_t)(k + 127) << 23);
+}
+
+// What the slots of max |q| and max |k| (fp32 bits) start from.  -LSE / scale enters the score
+// product in the copies' units and has to fit fp16 as well: |LSE| is at most ln of the keys of a
+// row above the largest score, which is below d * 8 * 8 = 8192 in those units, so ln(keys) / scale
+// may be 56000.  Where a caller's scale is smaller (1.5e-4 for 4096 keys), both copies
+// are held lower, as fp16_scale does for a max of 2^(2 + e).
+struct ScoreTops {
+  int32_t q, k;
+};
+inline ScoreTops score_tops(float scale, int64_t keys) {
+  const double over = std::log((double)keys) / (56000. * (double)scale);
+  const int t = over > 1. ? (int)std::ceil(std::log2(over)) : 0;
+  auto bits = [](int e) { return e ? 127 + 2 + e << 23 : 0; };
+  return {bits((t + 1) / 2), bits(t / 2)};
 }
 
 // s_waitcnt vmcnt(N) for a compile-time N.

@@ -268,7 +268,8 @@ struct RowUnit {
 // Clears the header of a windowed call (one workgroup of kPrepThreads): the lists are
 // empty, hold up to max_q and max_kv items and are run by grid_q and grid_kv workgroups.
 __device__ __forceinline__ void clear_win_header(int32_t *hdr, int grid_q, int64_t max_q,
-                                                 int grid_kv, int64_t max_kv) {
+                                                 int grid_kv, int64_t max_kv,
+                                                 const ScoreTops &tops = {0, 0}) {
   static_assert(kHdrSlots <= kPrepThreads, "a thread to a slot");
   const int tid = threadIdx.x;
   if (tid < kHdrSlots) {
@@ -279,6 +280,8 @@ __device__ __forceinline__ void clear_win_header(int32_t *hdr, int grid_q, int64
     }
     if (tid == kFwdQ + 2 * kXcds) v = (int)(max_q < INT32_MAX ? max_q : INT32_MAX);
     if (tid == kBwdQ + 2 * kXcds) v = (int)(max_kv < INT32_MAX ? max_kv : INT32_MAX);
+    if (tid == kMaxAbs) v = tops.q;
+    if (tid == kMaxAbs + 2) v = tops.k;
     __hip_atomic_store(&hdr[tid], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
 }
@@ -537,6 +540,7 @@ struct WinBwdPrep {
   int cus;
   BwdSplit *splits;     // dK / dV items cut into `parts` row ranges each (1: none)
   int parts;
+  ScoreTops tops;
 };
 // Row ranges of a dK / dV item.  A call of few key blocks and KV heads (4K tokens and 2 KV
 // heads: 66 items for 256 CUs) cuts each into as many as the CUs hold, of at least 2 row blocks

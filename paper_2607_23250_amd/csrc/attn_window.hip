@@ -59,7 +59,7 @@ void launch_win_prep_fwd(const WinPrep &p, hipStream_t st) {
 __global__ __launch_bounds__(kPrepThreads) void win_bwd_clear_kernel(WinPrep q, WinBwdPrep b,
                                                                      int grid_kv) {
   if (blockIdx.x == 0) {
-    clear_win_header(b.hdr, q.grid, q.max_items, grid_kv, b.max_items);
+    clear_win_header(b.hdr, q.grid, q.max_items, grid_kv, b.max_items, b.tops);
     return;
   }
   const int64_t i0 = (int64_t)(blockIdx.x - 1) * kPrepThreads + threadIdx.x;

@@ -8,7 +8,7 @@ collected by pytest).
   through the sums over a row that correct O, LSE and D, everything once more: four times in all.
 * fp16 numbers below 2^-14 lie 2^-24 apart, so P, dS and the copies of q, k, v and dout are also
   off by up to 2^-25 in the units of their scales: those bring max |dout| and max |v| to [1, 2)
-  and max |q| and max |k| below 8, or lower for a softmax_scale below 2^-10, by `down`.
+  and max |q| and max |k| below 8, or lower for a very small softmax_scale, by `down`.
 * fp32 and bf16 numbers below 2^-126 may become zero: a P, which loses P (dP - D), or a dS, each
   times scale |k| in dQ.  (dK and dV lose less than by the second point.)
 """
