@@ -1,5 +1,5 @@
 """GPU tests of libra_attn_bwd_ckpt8 besides its gradients at ordinary sizes: what it leaves in
-its workspace, and scores that the 8 bits move far."""
+its workspace, scores that the 8 bits move far, and dQ items cut into key ranges."""
 import numpy as np
 import pytest
 import torch
@@ -107,3 +107,34 @@ def test_large_scores(name, monkeypatch):
             value, bound = want[what]
             ref.close(what, got, (value, bound + 2.0 ** -23 * value.abs()))
     assert all(torch.equal(a, b) for a, b in zip(results[0], results[2]))
+
+
+CUT = {   # lengths, tiles, heads, d, window, sinks: few rows late in a long sample
+    "causal": ([40, 6000], blocks(6040, 512, 4, 2, [(5600, 6000)]), (4, 2), 128, 0, 0),
+    "causal_d64": ([5100], blocks(5100, 300, 3, ranges=[(4700, 5100)]), (3, 1), 64, 0, 0),
+    "window": ([2600, 40], blocks(2640, 300, 4, 2), (4, 2), 64, 2500, 3),
+    "window_far": ([7, 4000], blocks(4007, 512, 2, ranges=[(3500, 4007)]), (2, 1), 128, 1800, 5),
+}
+
+
+@pytest.mark.parametrize("name", CUT)
+def test_cut_dq_items(name, monkeypatch):
+    """dQ items cut into key ranges: the parts' merge takes D as it is, whatever the parts' sums
+    of dS, and (windowed) a cut item's first part writes the records of held q and dout."""
+    lengths, tiles, (h_q, h_kv), d, window, sinks = CUT[name]
+    say(f"[ckpt8 cut dQ {name}] lengths={lengths} heads=({h_q},{h_kv}) d={d} window={window}")
+    _, k, _, do, o, lse, held, cu, td = layer(5, lengths, tiles, h_q, h_kv, d, window, sinks)
+    rows, n_kv = do.shape[0], sum(lengths)
+    need = pl.libra_attn_bwd_ckpt8_workspace_size(len(tiles), len(lengths), rows, n_kv, h_q, h_kv,
+                                                  d, window=window, sinks=sinks)
+    ws = pl.alloc_workspace(need, DEV)
+    got = pl.libra_attn_bwd_ckpt8(*held, lse, do, cu, td, window=window, sinks=sinks,
+                                  workspace=ws)
+    assert int(ws[:4096].view(torch.int32)[60]) > 0   # items that were cut
+    q8, k8, v8, o8 = (pl.libra_ckpt8_unpack(*x, dtype=torch.float32).cpu() for x in held)
+    pairs = (ref.visible(lengths, ref.positions(tiles), n_kv, window, sinks),
+             ref.coverage(tiles, rows, h_q))
+    want = gradients(monkeypatch, q8, k8, v8, do.cpu(), pairs, d ** -0.5, lse.cpu(),
+                     (o8, lse.cpu()))
+    for what, x in zip(("dq", "dk", "dv"), got):
+        ref.close(what, x, want[what])
