@@ -120,10 +120,12 @@ CUT = {   # lengths, tiles, heads, d, window, sinks: few rows late in a long sam
 @pytest.mark.parametrize("name", CUT)
 def test_cut_dq_items(name, monkeypatch):
     """dQ items cut into key ranges: the parts' merge takes D as it is, whatever the parts' sums
-    of dS, and (windowed) a cut item's first part writes the records of held q and dout."""
+    of dS, and (windowed) a cut item's first part writes the records of held q and dout.  With
+    large channels those sums are not near zero: D corrected by them puts dK 8 bounds off."""
     lengths, tiles, (h_q, h_kv), d, window, sinks = CUT[name]
     say(f"[ckpt8 cut dQ {name}] lengths={lengths} heads=({h_q},{h_kv}) d={d} window={window}")
-    _, k, _, do, o, lse, held, cu, td = layer(5, lengths, tiles, h_q, h_kv, d, window, sinks)
+    _, _, _, do, _, lse, held, cu, td = layer(5, lengths, tiles, h_q, h_kv, d, window, sinks,
+                                            outliers(30.0))
     rows, n_kv = do.shape[0], sum(lengths)
     need = pl.libra_attn_bwd_ckpt8_workspace_size(len(tiles), len(lengths), rows, n_kv, h_q, h_kv,
                                                   d, window=window, sinks=sinks)
