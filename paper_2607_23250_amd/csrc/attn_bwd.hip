@@ -1365,7 +1365,7 @@ BwdLayout bwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, i
   L.bsplits = align256b(L.splits + (size_t)(L.max_parts / 2) * sizeof(FwdSplit));
   if (w) {
     // far samples lie side by side, so there are few of them
-    const int64_t far = win.sinks ? std::min(n, n_kv / ((int64_t)win.size + kFarRows + 1)) : 0;
+    const int64_t far = win_far_max(win, n, n_kv);
     const int64_t sinks = far * h_kv * sink_blocks(win);
     const int64_t slots = far ? sinks + kSinkParts : 0;
     L.far_list = align256b(L.bsplits + (size_t)sinks * sizeof(WinSink));

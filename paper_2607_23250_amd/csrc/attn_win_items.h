@@ -511,6 +511,23 @@ constexpr int kSinkPartRows = 32;
 constexpr int kSinkParts = 256;      // slots beyond one for each WinSink
 __host__ __device__ constexpr int sink_blocks(const Window &w) { return (w.sinks + 31) / 32; }
 __host__ __device__ constexpr size_t sink_part_floats(int d) { return (size_t)2 * 32 * d; }
+// The far samples of a call number at most min(n, n_kv / (size + far_rows + 1)), each with a
+// record and a slot of 64 d floats for 32 sinks of a KV head.  Many of them with many sinks would
+// take more than all else in the workspace (400 samples in 262144 keys, 8 KV heads, 1024 sinks, d =
+// 128: 3.4 GB), so there the line between far samples and others rises until the slots take no
+// more bytes than the fp16 copies of K and V (or 4096 slots, if those are more).  It rises only
+// where far samples are many, so those that it leaves out are short (that call, 16 query heads,
+// window 128: 9.6 ms with 256 rows for all, 5.6 so; 30 samples of 2000, 600 sinks: 2.24 and 2.26).
+inline int64_t win_far_max(const Window &w, int64_t n, int64_t n_kv) {
+  const int64_t fit = n_kv / ((int64_t)w.size + w.far_rows + 1);
+  return w.sinks ? (n < fit ? n : fit) : 0;
+}
+inline int32_t win_far_rows(const Window &w, int64_t n, int64_t n_kv, int h_kv) {
+  const int64_t copies = n_kv * h_kv / 64, room = copies > 4096 ? copies : 4096;
+  const int64_t most = w.sinks ? room / ((int64_t)h_kv * sink_blocks(w)) : 0;   // 2 or more
+  // n_kv / (size + far_rows + 1) <= most
+  return win_far_max(w, n, n_kv) <= most ? kFarRows : (int32_t)(n_kv / (most + 1) - w.size);
+}
 // First 128-key block in the window of the row at sample-local position p.
 __device__ __forceinline__ int first_key_block(int p, const Window &w) {
   return max(0, p - w.size + 1) / kBwdBK;
