@@ -71,17 +71,14 @@ int check_ws(const void *ws, size_t bytes, size_t need) {
   return LIBRA_OK;
 }
 
-// The window and sinks of a call, clamped to what the rows can reach, and its line between far
-// samples and others.
-int check_window(int64_t window, int64_t sinks, int64_t n, int64_t n_kv, int32_t h_kv,
-                 Window *out) {
+// The window and sinks of a call, clamped to what the rows can reach.
+int check_window(int64_t window, int64_t sinks, int64_t n_kv, Window *out) {
   if (window < 1) return fail(LIBRA_EINVAL, "window must be >= 1 (got %lld)", (long long)window);
   if (sinks < 0) return fail(LIBRA_EINVAL, "sinks must be >= 0 (got %lld)", (long long)sinks);
   if (sinks > kMaxSinks)
     return fail(LIBRA_EUNSUPPORTED, "%lld sinks (at most %d)", (long long)sinks, kMaxSinks);
   out->size = (int32_t)(window < n_kv ? window : n_kv);
   out->sinks = (int32_t)(sinks < n_kv ? sinks : n_kv);
-  out->far_rows = win_far_rows(*out, n, n_kv, h_kv);
   return LIBRA_OK;
 }
 
@@ -243,7 +240,7 @@ extern "C" size_t libra_attn_window_workspace_size(int64_t num_tiles, int64_t nu
                                                    int32_t backward) {
   Window win;
   if (num_tiles < 0 || check_sizes(num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim) ||
-      check_window(window, sinks, num_samples, n_kv_rows, h_kv, &win))
+      check_window(window, sinks, n_kv_rows, &win))
     return 0;
   if (backward)
     return bwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, win).total;
@@ -260,7 +257,7 @@ extern "C" int libra_attn_window_fwd(const void *q, const void *k, const void *v
   last_error_text().clear();
   Window win;
   if (int rc = check_sizes(num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim)) return rc;
-  if (int rc = check_window(window, sinks, num_samples, n_kv_rows, h_kv, &win)) return rc;
+  if (int rc = check_window(window, sinks, n_kv_rows, &win)) return rc;
   if (int rc = check_aligned({q, k, v, o}, lse, cu_seqlens, tiles)) return rc;
   return attn_fwd(q, k, v, cu_seqlens, num_samples, tiles, num_tiles, n_q_rows, n_kv_rows, h_q,
                   h_kv, head_dim, softmax_scale, o, lse, workspace, workspace_bytes, stream, win);
@@ -340,7 +337,7 @@ extern "C" int libra_attn_window_bwd(const void *q, const void *k, const void *v
   last_error_text().clear();
   Window win;
   if (int rc = check_sizes(num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim)) return rc;
-  if (int rc = check_window(window, sinks, num_samples, n_kv_rows, h_kv, &win)) return rc;
+  if (int rc = check_window(window, sinks, n_kv_rows, &win)) return rc;
   if (int rc = check_bwd(q, k, v, o, lse, dout, cu_seqlens, tiles, num_tiles, dq, dk, dv, flags))
     return rc;
   if (int rc = check_aligned({q, k, v, o, dout, dq, dk, dv}, lse, cu_seqlens, tiles)) return rc;
@@ -426,7 +423,7 @@ extern "C" size_t libra_attn_bwd_ckpt8_workspace_size(int64_t num_tiles, int64_t
                                                       int64_t sinks) {
   Window win;
   if (num_tiles < 0 || check_sizes(num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim) ||
-      ((window || sinks) && check_window(window, sinks, num_samples, n_kv_rows, h_kv, &win)))
+      ((window || sinks) && check_window(window, sinks, n_kv_rows, &win)))
     return 0;
   return ckpt8_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, win).total;
 }
@@ -444,7 +441,7 @@ extern "C" int libra_attn_bwd_ckpt8(const libra_ckpt8_t *q, const libra_ckpt8_t 
   Window win;
   if (int rc = check_sizes(num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim)) return rc;
   if (window || sinks)
-    if (int rc = check_window(window, sinks, num_samples, n_kv_rows, h_kv, &win)) return rc;
+    if (int rc = check_window(window, sinks, n_kv_rows, &win)) return rc;
   if (int rc = check_bwd(q, k, v, o, lse, dout, cu_seqlens, tiles, num_tiles, dq, dk, dv, flags))
     return rc;
   if (int rc = check_aligned({dout, dq, dk, dv}, lse, cu_seqlens, tiles)) return rc;

@@ -835,11 +835,10 @@ __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 
     if (idx < 0) break;
     const BwdItem item = items[idx];
     const int64_t key0 = cu[item.sample];
-    const int64_t full_len = cu[item.sample + 1] - key0;
     // keys past the last covered row get no gradient
-    const int64_t len = WIN ? (int64_t)samples[item.sample].ext : full_len;
-    const bool far = WIN && far_sample(win, full_len, n_kv - key0);   // its sinks' far rows are not walked here
-    const int near_sinks = far ? 0 : win.sinks;
+    const int64_t len = WIN ? (int64_t)samples[item.sample].ext : cu[item.sample + 1] - key0;
+    // the far rows of a far sample's sinks are not walked here
+    const int near_sinks = WIN && samples[item.sample].far >= 0 ? 0 : win.sinks;
     const int g = item.g;
     const int kloc0 = item.kb * kBwdBK;
     const int kw0 = kloc0 + 32 * w;                   // first key of this wave
@@ -1365,7 +1364,8 @@ BwdLayout bwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, i
   L.bsplits = align256b(L.splits + (size_t)(L.max_parts / 2) * sizeof(FwdSplit));
   if (w) {
     // far samples lie side by side, so there are few of them
-    const int64_t far = win_far_max(win, n, n_kv);
+    L.far_rows = win_far_rows(win, n, n_kv, h_kv);
+    const int64_t far = win_far_max(win, L.far_rows, n, n_kv);
     const int64_t sinks = far * h_kv * sink_blocks(win);
     const int64_t slots = far ? sinks + kSinkParts : 0;
     L.far_list = align256b(L.bsplits + (size_t)sinks * sizeof(WinSink));
@@ -1436,7 +1436,8 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
                       reinterpret_cast<BwdItem *>(ws + L.sink_items), cus,
                       reinterpret_cast<BwdSplit *>(ws + L.kv_splits),
                       win_kv_parts(win, L.max_blocks / h_kv, h_kv, cus),
-                      score_tops(scale, std::min(n_kv, (int64_t)win.size + win.sinks))};
+                      score_tops(scale, std::min(n_kv, (int64_t)win.size + win.sinks)),
+                      L.far_rows};
       launch_win_prep_bwd(WinPrep{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, win, hdr, qitems,
                                   L.max_qitems, 0, cus * kWinDqPerCu, cus * kWinDqPerCu,
                                   max_parts, splits}, wb, cus, st);

@@ -250,18 +250,11 @@ __device__ __forceinline__ int take_run_item(int32_t *hdr, int base, int q, int 
   }
 }
 
-// A sample whose rows reach this far past the window of its first key has the
-// gradients of its sink keys summed over those far rows by a kernel of their
-// own; in shorter ones the far rows are part of the sink keys' dK / dV items.
-// (Backward of 4096 tokens, 8 / 2 heads, window 256, 4 sinks: 196 us with 512, 157 with 256 and
-// 128; of 8192, 32 / 4 heads, window 512: 794 with 2048, 474, 449, 446.)
-constexpr int kFarRows = 256;
 // Windowed attention: the row at sample-local position p attends the keys
 // p - size + 1 .. p and the keys below `sinks` (both at most n_kv).
 struct Window {
   int32_t size = 0;    // 0: no window (plain causal attention)
   int32_t sinks = 0;
-  int32_t far_rows = kFarRows;   // or more (win_far_rows)
 };
 // An 8-bit checkpoint (ckpt8.hip): integers, and an exponent + 127 for each 32 of them.
 struct Held {
@@ -277,11 +270,6 @@ __device__ __forceinline__ bf16x8 held8(const Held &x, size_t at) {
   bf16x8 r;
   static_for<8>([&](auto i) { r[int(i)] = static_cast<bf16>((float)n[int(i)] * unit); });
   return r;
-}
-// Is a sample a far one?  `keys`: those from its first to the end of K, which the last may pass; the
-// workspace has room for the far samples that fit K side by side.
-__device__ __forceinline__ bool far_sample(const Window &w, int64_t len, int64_t keys) {
-  return w.sinks > 0 && (len < keys ? len : keys) > (int64_t)w.size + w.far_rows;
 }
 // The item walks its key blocks as steps: `far` blocks of sinks from key 0 on,
 // then, `gap` blocks later, those of the window.
@@ -763,7 +751,8 @@ struct BwdLayout {
          v16 = 0, stats = 0, splits = 0, bsplits = 0, cov = 0, parts = 0, total = 0;
   // windowed: WinSample records at ext, WinBlock at gmask, WinSink at bsplits
   size_t far_list = 0, sink_items = 0, sink_parts = 0, kv_splits = 0;
-  int64_t far = 0;   // far samples at most
+  int64_t far = 0;   // far samples at most, and their line (far_sample)
+  int far_rows = 0;
   int32_t max_parts = 0;   // split-K partial slots of the dQ kernel
   int64_t max_blocks = 0, max_items = 0, max_qitems = 0, nq_pad = 0;
 };

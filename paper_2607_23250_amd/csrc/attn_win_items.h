@@ -511,6 +511,18 @@ constexpr int kSinkPartRows = 32;
 constexpr int kSinkParts = 256;      // slots beyond one for each WinSink
 __host__ __device__ constexpr int sink_blocks(const Window &w) { return (w.sinks + 31) / 32; }
 __host__ __device__ constexpr size_t sink_part_floats(int d) { return (size_t)2 * 32 * d; }
+// A sample whose rows reach this far past the window of its first key has the
+// gradients of its sink keys summed over those far rows by a kernel of their
+// own; in shorter ones the far rows are part of the sink keys' dK / dV items.
+// (Backward of 4096 tokens, 8 / 2 heads, window 256, 4 sinks: 196 us with 512, 157 with 256 and
+// 128; of 8192, 32 / 4 heads, window 512: 794 with 2048, 474, 449, 446.)
+constexpr int kFarRows = 256;
+// Is a sample a far one?  `keys`: those from its first to the end of K, which the last may pass; the
+// workspace has room for the far samples that fit K side by side.
+__device__ __forceinline__ bool far_sample(const Window &w, int far_rows, int64_t len,
+                                           int64_t keys) {
+  return w.sinks > 0 && (len < keys ? len : keys) > (int64_t)w.size + far_rows;
+}
 // The far samples of a call number at most min(n, n_kv / (size + far_rows + 1)), each with a
 // record and a slot of 64 d floats for 32 sinks of a KV head.  Many of them with many sinks would
 // take more than all else in the workspace (400 samples in 262144 keys, 8 KV heads, 1024 sinks, d =
@@ -518,15 +530,16 @@ __host__ __device__ constexpr size_t sink_part_floats(int d) { return (size_t)2 
 // more bytes than the fp16 copies of K and V (or 4096 slots, if those are more).  It rises only
 // where far samples are many, so those that it leaves out are short (that call, 16 query heads,
 // window 128: 9.6 ms with 256 rows for all, 5.6 so; 30 samples of 2000, 600 sinks: 2.24 and 2.26).
-inline int64_t win_far_max(const Window &w, int64_t n, int64_t n_kv) {
-  const int64_t fit = n_kv / ((int64_t)w.size + w.far_rows + 1);
+inline int64_t win_far_max(const Window &w, int far_rows, int64_t n, int64_t n_kv) {
+  const int64_t fit = n_kv / ((int64_t)w.size + far_rows + 1);
   return w.sinks ? (n < fit ? n : fit) : 0;
 }
-inline int32_t win_far_rows(const Window &w, int64_t n, int64_t n_kv, int h_kv) {
+inline int win_far_rows(const Window &w, int64_t n, int64_t n_kv, int h_kv) {
   const int64_t copies = n_kv * h_kv / 64, room = copies > 4096 ? copies : 4096;
   const int64_t most = w.sinks ? room / ((int64_t)h_kv * sink_blocks(w)) : 0;   // 2 or more
   // n_kv / (size + far_rows + 1) <= most
-  return win_far_max(w, n, n_kv) <= most ? kFarRows : (int32_t)(n_kv / (most + 1) - w.size);
+  return win_far_max(w, kFarRows, n, n_kv) <= most ? kFarRows
+                                                   : (int)(n_kv / (most + 1) - w.size);
 }
 // First 128-key block in the window of the row at sample-local position p.
 __device__ __forceinline__ int first_key_block(int p, const Window &w) {
@@ -558,6 +571,7 @@ struct WinBwdPrep {
   BwdSplit *splits;     // dK / dV items cut into `parts` row ranges each (1: none)
   int parts;
   ScoreTops tops;
+  int far_rows;         // see far_sample
 };
 // Row ranges of a dK / dV item.  A call of few key blocks and KV heads (4K tokens and 2 KV
 // heads: 66 items for 256 CUs) cuts each into as many as the CUs hold, of at least 2 row blocks

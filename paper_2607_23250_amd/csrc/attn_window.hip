@@ -90,7 +90,7 @@ __device__ __forceinline__ void win_tile(const WinBwdPrep &a, int64_t t) {
     const int la = (int)((tl.q_begin > c0 ? tl.q_begin : c0) - c0);
     const int lb = (int)((tl.q_end < c1 ? tl.q_end : c1) - c0);
     if (la >= lb) return;   // rows past the last sample
-    const bool far = far_sample(a.win, c1 - c0, a.n_kv - c0);
+    const bool far = far_sample(a.win, a.far_rows, c1 - c0, a.n_kv - c0);
     WinSample &s = a.samples[j];
     if (first == 0) {
       atomicMax(&s.ext, lb);
@@ -224,7 +224,8 @@ __global__ __launch_bounds__(kPrepThreads) void win_kv_items_kernel(WinBwdPrep a
         const int kb = (int)(at - block_place(c0, lo));
         // rows up to the window of the last key; inline sinks: all
         const int64_t end = (int64_t)kb * kBwdBK + kBwdBK - 1 + a.win.size;
-        const bool all = kb * kBwdBK < a.win.sinks && !far_sample(a.win, len, a.n_kv - c0);
+        const bool all = kb * kBwdBK < a.win.sinks &&
+                         !far_sample(a.win, a.far_rows, len, a.n_kv - c0);
         it = BwdItem{(int32_t)lo, kb, g, -1, 0,
                      all || end > INT32_MAX ? INT32_MAX : (int32_t)end, b.t0, b.t1};
         has = 1;
