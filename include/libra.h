@@ -305,8 +305,10 @@ int libra_attn_bwd(const void *q, const void *k, const void *v, const void *o, c
  *       are out of range and the timing records: as in libra_attn_fwd and
  *       libra_attn_bwd.
  *   workspace: >= libra_attn_window_workspace_size bytes for the same window,
- *       sinks and direction, 256-byte aligned (0 bytes: invalid sizes).  For
- *       the backward's sinks it holds at most as much as fp16 copies of k and
+ *       sinks and direction, 256-byte aligned (0 bytes: invalid sizes).  A
+ *       forward's holds partial results only where items can be cut, for
+ *       single tokens at most 512 slots of 128 rows x (d + 2) fp32.  For the
+ *       backward's sinks it holds at most as much as fp16 copies of k and
  *       v, or 4096 slots of 64 * head_dim floats if those are more.
  * Single tokens: a tile may be one row.  For a batch of cached sequences,
  * cu_seqlens holds the sequences' places in k and v, and each has one tile of

@@ -174,7 +174,9 @@ int attn_fwd(const void *q, const void *k, const void *v, const int64_t *cu_seql
   if (!q || !k || !v || !cu_seqlens || !tiles || !o || !lse)
     return fail(LIBRA_EINVAL, "NULL tensor argument");
   const FwdLayout L =
-      fwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim);
+      win.size ? win_fwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim,
+                                win)
+               : fwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim);
   if (int rc = check_ws(workspace, workspace_bytes, L.total)) return rc;
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.f / std::sqrt((float)head_dim);
   int rc = LIBRA_OK;
@@ -244,7 +246,8 @@ extern "C" size_t libra_attn_window_workspace_size(int64_t num_tiles, int64_t nu
     return 0;
   if (backward)
     return bwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, win).total;
-  return fwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim).total;
+  return win_fwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, win)
+      .total;
 }
 
 extern "C" int libra_attn_window_fwd(const void *q, const void *k, const void *v,
@@ -277,7 +280,7 @@ extern "C" int libra_attn_fwd_noalloc(const void *q, const void *k, const void *
     return fail(LIBRA_EINVAL, "NULL tensor argument");
   // no split K here: its partial slots would not fit the scratch
   const FwdLayout L =
-      fwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, false);
+      fwd_layout(num_tiles, num_samples, n_q_rows, n_kv_rows, h_q, h_kv, head_dim, 0);
   if (L.total - L.items > kNoAllocListBytes)
     return fail(LIBRA_ENOSPC, "these sizes need a work-item list of %zu bytes, more than the %zu "
                 "of the built-in scratch; use libra_attn_fwd with a workspace",

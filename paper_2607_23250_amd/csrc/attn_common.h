@@ -757,10 +757,12 @@ struct BwdLayout {
   int64_t max_blocks = 0, max_items = 0, max_qitems = 0, nq_pad = 0;
 };
 
-// `split`: room for split-K partial results (libra_attn_fwd); without it the
-// forward never splits an item (the allocation-free entry point).
+// `parts`: slots for split-K partial results; without any the forward never splits
+// an item (the allocation-free entry point).
 FwdLayout fwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d,
-                     bool split = true);
+                     int parts = kFwdSplitSlots);
+FwdLayout win_fwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d,
+                         const Window &win);
 BwdLayout bwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d,
                      const Window &win = {});
 

@@ -389,13 +389,13 @@ int64_t fwd_max_items(int64_t T, int64_t n, int64_t n_q, int h_q, int h_kv) {
 }
 
 FwdLayout fwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d,
-                     bool split) {
+                     int parts) {
   FwdLayout L;
   L.max_items = fwd_max_items(T, n, n_q, h_q, h_kv);
   L.hdr = 0;
   L.items = kHdrBytes;
   L.splits = align256(L.items + (size_t)L.max_items * sizeof(FwdItem));
-  L.max_parts = split ? kFwdSplitSlots : 0;
+  L.max_parts = parts;
   // a split item has at least two parts
   L.parts = align256(L.splits + (size_t)(L.max_parts / 2) * sizeof(FwdSplit));
   L.total = align256(L.parts + (size_t)L.max_parts * fwd_part_floats(d) * sizeof(float));

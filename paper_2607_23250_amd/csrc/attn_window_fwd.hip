@@ -452,6 +452,30 @@ __global__ __launch_bounds__(256) void win_rows_combine_kernel(WinRows a,
     lse[(size_t)head * a.n_q + it.q_row0] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// Head chunks of a tile, and whether a call is one of single tokens.
+static int64_t row_chunks(int h_q, int h_kv) { return h_kv * ((h_q / h_kv + 3) / 4); }
+static bool row_call(int64_t T, int64_t n_q, int64_t jobs) {
+  return n_q <= T && jobs <= kMaxRowJobs;
+}
+// Key ranges of a single token's item at most, with `slots` for partial results in all.
+static int64_t row_cuts(const Window &win, int64_t n_kv, int64_t jobs, int64_t slots) {
+  const int64_t steps = win_max_steps(win, n_kv, 1);
+  return std::max<int64_t>(
+      1, std::min({steps / kRowMinSteps, (int64_t)kRowMaxCuts, slots / jobs}));
+}
+// A forward's workspace: slots only where its items can be cut, and for single tokens (512 ranges
+// fill the card) as many as they can have.
+FwdLayout win_fwd_layout(int64_t T, int64_t n, int64_t n_q, int64_t n_kv, int h_q, int h_kv, int d,
+                         const Window &win) {
+  const int64_t jobs = T * row_chunks(h_q, h_kv);
+  int64_t parts = win_may_split(win, n_kv) ? kFwdSplitSlots : 0;
+  if (jobs > 0 && row_call(T, n_q, jobs)) {
+    const int64_t cuts = row_cuts(win, n_kv, jobs, 512);
+    parts = cuts > 1 ? jobs * cuts : 0;
+  }
+  return fwd_layout(T, n, n_q, n_kv, h_q, h_kv, d, (int)parts);
+}
+
 // How a call without a list runs (parts, cuts); false: it has one.
 //   * Single tokens, no more Q rows than tiles: one unit for each key range, as many as run at
 //     once, two for each CU, and have slots for their partial results (32 / 8 heads, window
@@ -462,11 +486,9 @@ __global__ __launch_bounds__(256) void win_rows_combine_kernel(WinRows a,
 //     16.6 us with a list, 9.9 without).
 static bool without_list(WinRows &r, int max_parts, int cus) {
   const int64_t jobs = r.T * r.chunks;
-  if (r.n_q <= r.T && jobs <= kMaxRowJobs) {
-    const int64_t steps = win_max_steps(r.win, r.n_kv, 1);
-    const int64_t most = std::min<int64_t>(std::min<int64_t>(steps / kRowMinSteps, kRowMaxCuts),
-                                           std::min<int64_t>(max_parts, 2 * cus) / jobs);
-    r.cuts = r.parts = (int)std::max<int64_t>(most, 1);
+  if (row_call(r.T, r.n_q, jobs)) {
+    r.cuts = r.parts =
+        (int)row_cuts(r.win, r.n_kv, jobs, std::min<int64_t>(max_parts, 2 * cus));
     return true;
   }
   const int64_t windows = (r.n_q + kRows - 1) / kRows;
@@ -522,7 +544,7 @@ int launch_win_fwd(const void *q, const void *k, const void *v, const int64_t *c
                  hdr, h_q, h_kv, n_q, scale * kLog2e, static_cast<bf16 *>(o), lse,
                  reinterpret_cast<float *>(W + L.parts), win};
   const WinRows rows{cu, n, tiles, T, h_q, h_kv, n_q, n_kv, win, hdr,
-                     h_kv * ((h_q / h_kv + 3) / 4), 1, 1};
+                     (int)row_chunks(h_q, h_kv), 1, 1};
   auto *splits = reinterpret_cast<FwdSplit *>(W + L.splits);
   return (d == 128 ? launch_win_fwd_d<128> : launch_win_fwd_d<64>)(a, rows, L, splits, st, tm);
 }

@@ -28,3 +28,24 @@ def test_far_rows_of_few_samples():
     for window in (1, 500):
         one = backward(1, 1 << 20, 8, 128, window, 64) - backward(1, 1 << 20, 8, 128, window, 0)
         assert one >= (16 + 256) * 64 * 128 * 4
+
+
+@pytest.mark.parametrize("tiles,rows,keys,h_q,h_kv,window,slots", [
+    (16, 4096, 4096, 32, 8, 64, 0),               # items of a few key blocks
+    (1, 1, 60, 8, 2, 4096, 0),                    # a token of one key block
+    (600, 600, 600 * 5000, 8, 2, 4096, 0),        # more tokens than run at once
+    (64, 64, 64 * 6000, 32, 8, 4096, 0),          # 512 items of whole tokens
+    (32, 32, 32 * 6000, 32, 8, 4096, 512),        # two key ranges for each of 256
+    (1, 1, 1 << 20, 8, 2, 1 << 20, 128),          # 64 for each of 2
+    (16, 4096, 4096, 32, 8, 4096, 3072),          # a list of long items
+])
+@pytest.mark.parametrize("d", [64, 128])
+def test_forward_has_slots_only_where_items_are_cut(tiles, rows, keys, h_q, h_kv, window, slots, d):
+    """Beyond what the same call takes with items of a single key block: slots of 128 rows of d + 2
+    floats, half as many records of 64 bytes, alignment."""
+    def size(w):
+        return pl.libra_attn_window_workspace_size(tiles, tiles, rows, keys, h_q, h_kv, d, False,
+                                                   window=w, sinks=4)
+    more = size(window) - size(1)
+    slot = 128 * (d + 2) * 4
+    assert slots * slot <= more <= slots * (slot + 32) + 512
