@@ -7,7 +7,9 @@
 // 255 marks a group with an infinity or a NaN, which comes back as 32 NaN.  Every step is
 // exact but the one rounding (products with powers of two, and integers of 7 bits fit a
 // bf16's 8), so the result depends on nothing but x, and an unpacked value is off by at most
-// half a unit, 2^-7 of the group's largest element.
+// half a unit.  That is 2^-7 of the group's largest element or less, but for groups whose largest is
+// below 64 units of 2^-126, which may be lost whole; and values above 127 units of 2^121 are off
+// by up to one of them.
 //
 // Both directions move 16 elements to a thread (whole 16-byte pieces of the 8-bit side) and
 // are bound by memory: [32768][32][128] bf16, 814 MB packed and unpacked again in 158 us,
