@@ -325,6 +325,9 @@ int libra_attn_bwd(const void *q, const void *k, const void *v, const void *o, c
  * single tokens, with 4 blocks or more.  dK / dV of sink keys are summed over
  * parts of a long sample's rows, in row order.
  * Results are the same from one call to the next.
+ * libra_plan knows no window: its tile costs are causal pairs, so tiles of a
+ * long sample that are to run under a window are placed as heavier than they
+ * are.
  */
 size_t libra_attn_window_workspace_size(int64_t num_tiles, int64_t num_samples, int64_t n_q_rows,
                                         int64_t n_kv_rows, int32_t h_q, int32_t h_kv,

@@ -30,7 +30,7 @@ def score_error(q, k, scale, pairs):
     for h in range(q.shape[1]):
         rows = torch.nonzero(cov[:, h] & ok.any(1))[:, 0]
         s = (q[rows, h].double().abs() @ k[:, h // G].double().abs().T) * ok[rows]
-        most = max(most, float(s.max()) * scale)
+        most = max(most, float(s.max()) * scale) if len(rows) else most
     return 4 * (q.shape[2] + 16) * 2.0 ** -24 * (2 * most + math.log(k.shape[0]))
 
 
