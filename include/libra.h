@@ -325,6 +325,8 @@ int libra_attn_bwd(const void *q, const void *k, const void *v, const void *o, c
  * single tokens, with 4 blocks or more.  dK / dV of sink keys are summed over
  * parts of a long sample's rows, in row order.
  * Results are the same from one call to the next.
+ * Precision: the backward's dQ products take the fp16 copies too (libra_attn_bwd:
+ * bf16), so that dS rounds to 11 bits.
  * libra_plan knows no window: its tile costs are causal pairs, so tiles of a
  * long sample that are to run under a window are placed as heavier than they
  * are.
@@ -386,9 +388,9 @@ typedef struct libra_ckpt8 {
  * D = rowsum(dO * O), for dQ and for dK alike (libra_attn_bwd, whose O and LSE
  * belong to its q, k and v, corrects D by the sums of dS; here the rows of P
  * need not sum to 1).
- * Nor is P bounded by 1: where it or dS passes the range of fp16, the dK / dV
- * products concerned are formed again with P and dS in bf16 pairs (16 bits, the
- * range of fp32, past which a gradient is infinite or NaN).
+ * Nor is P bounded by 1: where it or dS passes the range of fp16, the products
+ * concerned are formed again with P and dS in bf16 pairs (16 bits, the range of
+ * fp32, past which a gradient is infinite or NaN).
  *   lse: fp32, of the forward on the values before packing.
  *   workspace: >= libra_attn_bwd_ckpt8_workspace_size bytes, 256-byte aligned
  *       (a backward's workspace, then the unpacked tensors).

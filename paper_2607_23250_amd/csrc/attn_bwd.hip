@@ -1481,8 +1481,8 @@ static int launch_bwd_d(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 
     int rc;
     if constexpr (WIN) {
       if (tm_q) hipEventRecord(tm_q->begin, st);
-      rc = launch_win_dq(D, WinDq{q, o, dout, k, v, q8, o8, lse, qitems, hdr, h_q, h_kv, n_q,
-                                  L.nq_pad, scale, scale * kLog2e, d_fix, win, dq, rec, stats,
+      rc = launch_win_dq(D, WinDq{q, o, dout, k16, v16, q8, o8, lse, qitems, hdr, h_q, h_kv, n_q,
+                                  L.nq_pad, scale, scale * kLog2e, win, dq, rec, stats,
                                   parts}, cus, st);
       if (max_parts > 0)
         launch_dq_combine(D, splits, hdr, parts, stats, h_q, L.nq_pad, scale, dq, rec, d_fix,

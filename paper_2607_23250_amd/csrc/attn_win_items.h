@@ -605,14 +605,15 @@ constexpr int64_t kMaxSmallUnits = 4096;
 
 // Arguments of the windowed dQ kernel (attn_window_dq.hip).  q and o, or q8 and o8.
 struct WinDq {
-  const bf16 *q, *o, *dout, *k, *v;
+  const bf16 *q, *o, *dout;
+  const f16 *k16, *v16;
   Held q8, o8;
   const float *lse;
   const FwdItem *items;
   int32_t *hdr;
   int h_q, h_kv;
   int64_t n_q, nq_pad;
-  float scale, c2, d_fix;   // d_fix: see attn_bwd_dq.hip
+  float scale, c2;
   Window win;
   bf16 *dq;
   f16 *rec;

@@ -8,7 +8,8 @@ collected by pytest).
   through the sums over a row that correct O, LSE and D, everything once more: four times in all.
 * fp16 numbers below 2^-14 lie 2^-24 apart, so P, dS and the copies of q, k, v and dout are also
   off by up to 2^-25 in the units of their scales: those bring max |dout| and max |v| to [1, 2)
-  and max |q| and max |k| below 8, or lower for a very small softmax_scale, by `down`.
+  and max |q| and max |k| below 8, or lower for a very small softmax_scale, by `down`.  (The
+  windowed dQ forms its dS times 16.)
 * fp32 and bf16 numbers below 2^-126 may become zero: a P, which loses P (dP - D), or a dS, each
   times scale |k| in dQ.  (dK and dV lose less than by the second point.)
 """
@@ -40,7 +41,7 @@ def underflow(q, k, v, do, pairs, scale, lse, down=1.0):
     n_kv, h_kv, d = k.shape
     G = q.shape[1] // h_kv
     q, k, v, do, lse = (x.double() for x in (q, k, v, do, lse))
-    top_q = max(1.0, float(q.abs().max()) / 4) * down
+    top_q, top_k = (max(1.0, float(x.abs().max()) / 4) * down for x in (q, k))
     top_o, top_v = float(do.abs().max()), float(v.abs().max())
     dq, dk, dv = (torch.zeros(x.shape, dtype=torch.float64) for x in (q, k, v))
     for h in range(q.shape[1]):
@@ -55,7 +56,9 @@ def underflow(q, k, v, do, pairs, scale, lse, down=1.0):
         dk[:, g] += STEP * scale * (
             (top_o * top_v * (seen + 2 * d * P)).T @ Q.abs()
             + (P * size).sum(0)[:, None] * top_q)
-        dq[rows, h] = 2.0 ** -126 * scale * (((1 + size) * seen) @ k[:, g].abs())
+        dq[rows, h] = scale * (
+            ((2.0 ** -126 * (1 + size) + STEP / 16 * top_o * top_v) * seen + STEP * 2 * d * top_o
+             * top_v * P) @ k[:, g].abs() + STEP * top_k * (P * size).sum(1, keepdim=True))
     return {"dq": dq, "dk": dk, "dv": dv}
 
 
