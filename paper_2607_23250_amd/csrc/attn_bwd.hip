@@ -571,7 +571,7 @@ __device__ __forceinline__ void kv_pass(unsigned block, unsigned blocks,
   float mk = 0.f, mv = 0.f, s_k = 1.f, s_v = 1.f;
   if constexpr (CONVERT) {
     s_k = fp16_scale((uint32_t)hdr[kMaxAbs + 2], false);
-    s_v = fp16_scale((uint32_t)hdr[kMaxAbs + 3], true);
+    s_v = fp16_scale(top_v(hdr), true);
   }
   int64_t lo = 0, hi = 0, end = 0;   // rows [lo, hi) of the current sample; loaded keys end at `end`
   int64_t from = 0, sink_end = 0;    // WIN: and start at `from`, but for those before sink_end
@@ -757,6 +757,7 @@ __global__ __launch_bounds__(256) void bwd_max_kernel(BwdPass a) {
 template <int D, bool WIN>
 __global__ __launch_bounds__(256) void bwd_copy_kernel(BwdPass a) {
   const unsigned b = blockIdx.x;
+  if (b == 0 && threadIdx.x == 0) a.hdr[kTopV] = (int32_t)top_v(a.hdr);   // for the kernels after it
   if (b < a.kv_blocks)
     kv_pass<D, true, WIN>(b, a.kv_blocks, a.k, a.v, a.cu, a.n, a.ext, a.h_kv, a.n_kv, a.hdr,
                           a.k16, a.v16, a.win);
@@ -818,7 +819,7 @@ __global__ __launch_bounds__(kThreads, 1) __attribute__((amdgpu_waves_per_eu(1, 
   const float s_q = fp16_scale((uint32_t)hdr[kMaxAbs + 0], false);
   const float s_o = fp16_scale((uint32_t)hdr[kMaxAbs + 1], true);
   const float s_k = fp16_scale((uint32_t)hdr[kMaxAbs + 2], false);
-  const float s_v = fp16_scale((uint32_t)hdr[kMaxAbs + 3], true);
+  const float s_v = fp16_scale((uint32_t)hdr[kTopV], true);
   const float c2s = c2 / (s_q * s_k);
   const float dk_mul = scale / (s_q * s_o * s_v), dv_mul = 1.f / s_o;
 
@@ -1285,7 +1286,7 @@ __global__ __launch_bounds__(256) void bwd_dkdv_combine_kernel(
   const int count = hdr[kBwdSplits] * kCombineSplit;
   const float s_q = fp16_scale((uint32_t)hdr[kMaxAbs + 0], false);
   const float s_o = fp16_scale((uint32_t)hdr[kMaxAbs + 1], true);
-  const float s_v = fp16_scale((uint32_t)hdr[kMaxAbs + 3], true);
+  const float s_v = fp16_scale((uint32_t)hdr[kTopV], true);
   const float mul[2] = {scale / (s_q * s_o * s_v), 1.f / s_o};   // as in the kernel
   const int tid = threadIdx.x, col = (tid % kCombineThreads) * W;
   for (int e = blockIdx.x; e < count; e += gridDim.x) {

@@ -70,7 +70,7 @@ __global__ __launch_bounds__(2 * kThreads, 1) void attn_bwd_dq_kernel(
   const int q_serve = blockIdx.x % kXcds;
   int q_state = kTakeFirst;
   const float s_ov = fp16_scale((uint32_t)hdr[kMaxAbs + 1], true) *
-                     fp16_scale((uint32_t)hdr[kMaxAbs + 3], true);
+                     fp16_scale((uint32_t)hdr[kTopV], true);
   // staging: wave load u fills unit wv + 8 u of a tile
   uint32_t k_lane[S::NK];
   static_for<S::NK>([&](auto u) {
@@ -364,7 +364,7 @@ __global__ __launch_bounds__(256) void bwd_dq_combine_kernel(
   constexpr int W = D / kCombineThreads;   // columns of a thread
   const int count = hdr[kFwdSplits] * kCombineSplit;
   const float s_ov = fp16_scale((uint32_t)hdr[kMaxAbs + 1], true) *
-                     fp16_scale((uint32_t)hdr[kMaxAbs + 3], true);
+                     fp16_scale((uint32_t)hdr[kTopV], true);
   const int tid = threadIdx.x, col = (tid % kCombineThreads) * W;
   for (int e = blockIdx.x; e < count; e += gridDim.x) {
     const FwdSplit sp = splits[e / kCombineSplit];

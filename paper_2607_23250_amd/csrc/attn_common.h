@@ -46,6 +46,7 @@ constexpr int kPrepThreads = 1024;
 // [base+8, base+16) and segment starts at [base+16, base+24); its queue heads
 // are at head_slot(base, queue).
 enum HdrSlot {
+  kTopV = 3,       // backward: max |V| as its scale counts it (top_v)
   kBadTiles = 4,   // tiles skipped because they were out of range (+1 on item overflow)
   kOddHeads = 5,   // backward: some tile covers an odd number of a KV group's heads
   kBwdSplits = 6,  // backward: split dK / dV items (BwdSplit records)
@@ -661,6 +662,14 @@ __host__ __device__ __forceinline__ float fp16_scale(uint32_t mx, bool up) {
   int k = up ? -e : (e > 2 ? -(e - 2) : 0);
   k = k < -126 ? -126 : (k > 126 ? 126 : k);
   return __builtin_bit_cast(float, (uint32_t)(k + 127) << 23);
+}
+// What the scale of V counts as its max, from those of dO and V: more where the product of the
+// scales, by which dP and D are multiplied, would pass fp32 (max |dO| max |V| below 2^-120).
+__device__ __forceinline__ uint32_t top_v(const int32_t *hdr) {
+  const int o = (int)(__float_as_uint(fp16_scale((uint32_t)hdr[kMaxAbs + 1], true)) >> 23) - 127;
+  const uint32_t least = (uint32_t)max(0, 127 + o - 120) << 23;   // 2^(o - 120)
+  const uint32_t v = (uint32_t)hdr[kMaxAbs + 3];
+  return v && v < least ? least : v;
 }
 
 // What the slots of max |q| and max |k| (fp32 bits) start from.  -LSE / scale enters the score

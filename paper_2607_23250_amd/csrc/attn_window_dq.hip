@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kThreads, 2) void win_dq_kernel(WinDq a) {
   const float s_q = fp16_scale((uint32_t)hdr[kMaxAbs + 0], false);
   const float s_o = fp16_scale((uint32_t)hdr[kMaxAbs + 1], true);
   const float s_k = fp16_scale((uint32_t)hdr[kMaxAbs + 2], false);
-  const float s_v = fp16_scale((uint32_t)hdr[kMaxAbs + 3], true);
+  const float s_v = fp16_scale((uint32_t)hdr[kTopV], true);
   const float s_ov = s_o * s_v, c2s = a.c2 / (s_q * s_k);   // S comes out times s_q s_k, dP s_o s_v
   // P is formed times 16: P |dP - D| is below 2^11 in these units, and small terms stay further
   // from the smallest fp16 numbers.
