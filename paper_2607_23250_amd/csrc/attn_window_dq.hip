@@ -13,9 +13,9 @@
 // results while the other computes.  Each wave takes both 32-key halves of a block for its
 // (query head, 32 rows); halves that no row of the wave attends are passed over.  With one
 // workgroup of eight waves per CU, as in the causal kernel, every CU waited about 10 of an
-// item's 36 us for its rows: 1146 us for 32K tokens, 32 heads, window 1024, now 870.
-// Bound by the three products (741 GFLOP there, 850 TFLOP/s) at the clock that the card
-// holds under them: the matrix cores are busy half of the cycles, at 1.77 GHz.
+// item's 36 us for its rows: 1146 us for 32K tokens, 32 heads, window 1024, now 879 (870 with
+// bf16 products).  Bound by the three products (741 GFLOP there, 843 TFLOP/s) at the clock that
+// the card holds under them: the matrix cores are busy half of the cycles, at 1.75 GHz.
 //
 // The kernel also does what the causal calls leave to a pass of its own over Q, O and dO:
 // D = rowsum(dO O), and the records of the dK / dV kernel (see pre_pass in attn_bwd.hip for

@@ -14,9 +14,9 @@
 // P is rounded to bf16 for its product with V, whose type it shares; the running max, the
 // row sum and O stay in fp32, and the sum takes P before the rounding.
 // Bound by the matrix cores' share of the cycles and the clock under them (a 32K pack, 32
-// heads, window 1024: 614 us, 805 TFLOP/s, busy 42% at 1.88 GHz; the 256K share, window 4096:
-// 1790 to 1850 us, 1.03 PFLOP/s, 53% at 1.62); single tokens (WinRows) by reading K and V
-// (64 sequences of 6000 keys, 8 KV heads, window 4096: 180 us, 5.5 TB/s).
+// heads, window 1024: 603 us, 819 TFLOP/s, busy 42% at 1.86 GHz; the 256K share, window 4096:
+// 1787 to 1850 us, 1.03 PFLOP/s, 53% at 1.64); single tokens (WinRows) by reading K and V
+// (64 sequences of 6000 keys, 8 KV heads, window 4096: 181 us, 5.5 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
