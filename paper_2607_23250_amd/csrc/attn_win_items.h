@@ -517,8 +517,8 @@ __host__ __device__ constexpr size_t sink_part_floats(int d) { return (size_t)2 
 // (Backward of 4096 tokens, 8 / 2 heads, window 256, 4 sinks: 196 us with 512, 157 with 256 and
 // 128; of 8192, 32 / 4 heads, window 512: 794 with 2048, 474, 449, 446.)
 constexpr int kFarRows = 256;
-// Is a sample a far one?  `keys`: those from its first to the end of K, which the last may pass; the
-// workspace has room for the far samples that fit K side by side.
+// Is a sample a far one?  `keys`: those from its first to the end of K, which the last may pass;
+// the workspace has room for the far samples that fit K side by side.
 __device__ __forceinline__ bool far_sample(const Window &w, int far_rows, int64_t len,
                                            int64_t keys) {
   return w.sinks > 0 && (len < keys ? len : keys) > (int64_t)w.size + far_rows;

@@ -37,7 +37,6 @@ def test_far_rows_of_few_samples():
     (64, 64, 64 * 6000, 32, 8, 4096, 0),          # 512 items of whole tokens
     (32, 32, 32 * 6000, 32, 8, 4096, 512),        # two key ranges for each of 256
     (1, 1, 1 << 20, 8, 2, 1 << 20, 128),          # 64 for each of 2
-    (16, 4096, 4096, 32, 8, 4096, 3072),          # a list of long items
 ])
 @pytest.mark.parametrize("d", [64, 128])
 def test_forward_has_slots_only_where_items_are_cut(tiles, rows, keys, h_q, h_kv, window, slots, d):
@@ -49,3 +48,11 @@ def test_forward_has_slots_only_where_items_are_cut(tiles, rows, keys, h_q, h_kv
     more = size(window) - size(1)
     slot = 128 * (d + 2) * 4
     assert slots * slot <= more <= slots * (slot + 32) + 512
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_forward_of_a_list_of_long_items(d):
+    """As much as libra_attn_fwd asks for, whose items can be cut too."""
+    sizes = (16, 2, 4096, 4096, 32, 8, d)
+    assert pl.libra_attn_window_workspace_size(*sizes, False, window=4096, sinks=4) \
+        == pl.libra_attn_workspace_size(*sizes, False)
