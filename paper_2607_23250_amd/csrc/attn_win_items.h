@@ -528,8 +528,9 @@ __device__ __forceinline__ bool far_sample(const Window &w, int far_rows, int64_
 // take more than all else in the workspace (400 samples in 262144 keys, 8 KV heads, 1024 sinks, d =
 // 128: 3.4 GB), so there the line between far samples and others rises until the slots take no
 // more bytes than the fp16 copies of K and V (or 4096 slots, if those are more).  It rises only
-// where far samples are many, so those that it leaves out are short (that call, 16 query heads,
-// window 128: 9.6 ms with 256 rows for all, 5.6 so; 30 samples of 2000, 600 sinks: 2.24 and 2.26).
+// where far samples and sinks are many: then most keys of the samples that it leaves out are sinks,
+// and an item of 128 keys is the better form for them (that call, 16 query heads, window 128: 9.6
+// ms with 256 rows for all, 5.6 so; 60 samples of 2000, window 8, 1024 sinks: 7.1 and 4.0).
 inline int64_t win_far_max(const Window &w, int far_rows, int64_t n, int64_t n_kv) {
   const int64_t fit = n_kv / ((int64_t)w.size + far_rows + 1);
   return w.sinks ? (n < fit ? n : fit) : 0;
